@@ -365,6 +365,80 @@ sd2_status sd2_accept_logits_noalloc(const void* d_target, const void* d_draft, 
  * reports the last call only. */
 sd2_status sd2_accept_logits_noalloc_check(void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * A shared paged cache: prompt attention, appending rows, forking sequences, compacting the pool.
+ * (Additions of this library: the paper has no counterpart.) The pool is that of sd2_attention,
+ * bf16 [L][n_blocks][2 (K, V)][Hkv][16][hd]; a page id names the same block of every layer. A
+ * sequence is a row of a table of page ids and a length; a batch of new rows is packed: rows
+ * d_cu_rows[s] .. d_cu_rows[s+1] - 1 are the n_s last positions of sequence s, the last of them at
+ * position d_kv_len[s] - 1 (d_cu_rows [n_seq + 1] starts at 0 and does not fall). All of these are
+ * device memory, read on the given stream; no call waits for the GPU or allocates device memory.
+ * d_err (may be null): a device word or-ed with 2 (a wait timed out), 4 (a page id, parent or
+ * position out of range: the entry is skipped) or 8 (the pool has too few free pages).
+ * ------------------------------------------------------------------------------------------- */
+
+/* Causal grouped-query attention of packed prompt rows over the paged cache, the rows' own K/V
+ * included (append them first): row i of sequence s, at position p = d_kv_len[s] - n_s + i, gives
+ *   out = sum_{j <= p} softmax_j(q . k_j / sqrt(hd)) v_j,   lse = ln sum_{j <= p} exp(q . k_j / sqrt(hd)).
+ *   d_q bf16, row m's H heads of hd at d_q + m * ldq (ldq >= H * hd, a multiple of 8); d_out bf16
+ *   [M, H * hd]; d_lse f32 [M, H] or null. hd 64 or 128; H a multiple of Hkv, H / Hkv <= 128.
+ * A row with p < 0 sees nothing: out 0, lse -inf. Rows at or beyond d_cu_rows[n_seq] are not written.
+ * Positions at or beyond min(d_kv_len[s], 16 * bt_stride) are not read, whatever their page holds;
+ * those below it must hold finite values. max_kv >= every d_kv_len[s] lets the call cut long caches
+ * into splits where there are few rows (it sizes the split only: a larger length is still right).
+ * d_workspace: sd2_attention_prompt_workspace_bytes(M, n_seq, H, Hkv, hd, max_kv) bytes, 256-byte
+ * aligned; contents need not be initialised; calls whose GPU work overlaps must not share it.
+ * Errors: SD2_EINVAL (null, shape, alignment, workspace too small), SD2_ECUDA. */
+size_t sd2_attention_prompt_workspace_bytes(int32_t M, int32_t n_seq, int32_t H, int32_t Hkv, int32_t hd,
+                                            int32_t max_kv);
+sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t H, int32_t Hkv, int32_t hd,
+                                const void* d_pool, int32_t n_blocks, const int32_t* d_table, int32_t bt_stride,
+                                int32_t layer, const int32_t* d_cu_rows, const int32_t* d_kv_len, int32_t n_seq,
+                                int32_t max_kv, void* d_out, float* d_lse, void* d_workspace, size_t workspace_bytes,
+                                uint32_t* d_err, void* stream);
+
+/* Write packed K and V rows (rotary embedding applied by the caller) to their pages of `layer`:
+ * row m's Hkv heads of hd are at d_k + m * ldk and d_v + m * ldv, f32 (rounded to the nearest bf16) or
+ * bf16, 16-byte aligned rows. A row whose position lies outside [0, 16 * bt_stride) is skipped. The
+ * pages written must belong to one sequence alone (sd2_pages_fork sees to it). hd a multiple of 8. */
+sd2_status sd2_pages_append(const void* d_k, int64_t ldk, const void* d_v, int64_t ldv, int32_t dtype, int32_t M,
+                            int32_t Hkv, int32_t hd, void* d_pool, int32_t n_blocks, const int32_t* d_table,
+                            int32_t bt_stride, int32_t layer, const int32_t* d_cu_rows, const int32_t* d_kv_len,
+                            int32_t n_seq, uint32_t* d_err, void* stream);
+
+/* A new batch of sequences out of an old one: fork, drop, roll back and extend in one call. New
+ * sequence b holds the first keep = min(d_keep[b], d_len[p]) positions of old sequence p = d_parent[b]
+ * (d_keep null: all; p = -1: none) and room for d_grow[b] positions after them (null: none), at most
+ * bt_stride pages. Pages it holds whole are shared. A partial last page stays with its lowest-numbered
+ * holder if no sequence holds it whole and it is not pinned; every other holder gets a page of its own
+ * with the rows below keep copied, in all L layers. Pages that nobody holds any more are free.
+ *   d_table [n_seq, bt_stride], d_len [n_seq]; d_pinned [n_blocks] (may be null): holders outside the
+ *   table, whose pages are neither granted nor appended to. Outputs, none of them an input: d_table_out
+ *   [n_out, bt_stride] (unused entries 0), d_len_out [n_out], d_pages_out [n_out] (pages held), d_ref_out
+ *   [n_blocks] (holders of each page, pinned ones included; 0: free).
+ * New pages are the lowest free ids, granted in the order of b. When they run out (d_err bit 8) a
+ * sequence without a page for its tail is cut to its whole pages, and the room ends with d_pages_out.
+ * d_workspace: sd2_pages_fork_workspace_bytes(n_out, n_blocks) bytes, 256-byte aligned, contents need
+ * not be initialised. Work that still reads the freed pages must come before this call on its stream. */
+size_t sd2_pages_fork_workspace_bytes(int32_t n_out, int32_t n_blocks);
+sd2_status sd2_pages_fork(void* d_pool, int32_t L, int32_t n_blocks, int32_t Hkv, int32_t hd, const int32_t* d_table,
+                          int32_t bt_stride, const int32_t* d_len, int32_t n_seq, const int32_t* d_parent,
+                          const int32_t* d_keep, const int32_t* d_grow, const int32_t* d_pinned, int32_t n_out,
+                          int32_t* d_table_out, int32_t* d_len_out, int32_t* d_pages_out, int32_t* d_ref_out,
+                          void* d_workspace, size_t workspace_bytes, uint32_t* d_err, void* stream);
+
+/* Move the N live pages (d_ref > 0) to ids 0 .. N - 1, in all L layers: the j-th lowest free id below N
+ * takes the j-th lowest live page at or above it, the others stay. d_pages [n_seq]: entries in use of
+ * each table row. Outputs: d_table_out (entries renamed, unused ones 0; may be d_table), d_ref_out
+ * (not d_ref), d_map [n_blocks] (a page's new id, -1 for a free one), d_n_live [1] = N.
+ * d_workspace: sd2_pages_compact_workspace_bytes(n_blocks) bytes, 256-byte aligned, contents need not
+ * be initialised. */
+size_t sd2_pages_compact_workspace_bytes(int32_t n_blocks);
+sd2_status sd2_pages_compact(void* d_pool, int32_t L, int32_t n_blocks, int32_t Hkv, int32_t hd, const int32_t* d_table,
+                             int32_t bt_stride, const int32_t* d_pages, int32_t n_seq, const int32_t* d_ref,
+                             int32_t* d_table_out, int32_t* d_ref_out, int32_t* d_map, int32_t* d_n_live,
+                             void* d_workspace, size_t workspace_bytes, uint32_t* d_err, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

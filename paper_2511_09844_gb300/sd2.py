@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 import torch
 
@@ -31,7 +31,8 @@ EXPORTS = ["sd2_init", "sd2_prefill", "sd2_step", "sd2_accept", "sd2_check", "sd
            "sd2_set_drafter_chain", "sd2_attention", "sd2_set_fused_attention",
            "sd2_accept_logits_noalloc_check", "sd2_debug_fail_alloc", "sd2_debug_expire_wait",
            "sd2_gemm_timing", "sd2_gemm_timing_read", "sd2_generate", "sd2_attention_flat_workspace_bytes",
-           "sd2_attention_flat"]
+           "sd2_attention_flat", "sd2_attention_prompt_workspace_bytes", "sd2_attention_prompt", "sd2_pages_append",
+           "sd2_pages_fork_workspace_bytes", "sd2_pages_fork", "sd2_pages_compact_workspace_bytes", "sd2_pages_compact"]
 
 
 class LMConfig(ctypes.Structure):
@@ -115,9 +116,28 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sd2_gemm_timing_read.argtypes = [c_void_p, c_int32, POINTER(c_int32), POINTER(c_uint64), POINTER(c_double),
                                          POINTER(c_int32)]
     lib.sd2_debug_expire_wait.argtypes = [c_void_p, c_int64]
+    lib.sd2_attention_prompt_workspace_bytes.argtypes = [c_int32] * 6
+    lib.sd2_attention_prompt_workspace_bytes.restype = c_size_t
+    lib.sd2_attention_prompt.argtypes = [c_void_p, c_int64, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int32,
+                                         c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_void_p,
+                                         c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
+    lib.sd2_pages_append.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_int32, c_int32, c_int32, c_void_p,
+                                     c_int32, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_void_p,
+                                     c_void_p]
+    lib.sd2_pages_fork_workspace_bytes.argtypes = [c_int32, c_int32]
+    lib.sd2_pages_fork_workspace_bytes.restype = c_size_t
+    lib.sd2_pages_fork.argtypes = [c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_int32,
+                                   c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                   c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
+    lib.sd2_pages_compact_workspace_bytes.argtypes = [c_int32]
+    lib.sd2_pages_compact_workspace_bytes.restype = c_size_t
+    lib.sd2_pages_compact.argtypes = [c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int32, c_void_p,
+                                      c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,
+                                      c_void_p, c_void_p]
     for name in EXPORTS:
         if name not in ("sd2_last_error", "sd2_accept_workspace_bytes", "sd2_steer_workspace_bytes",
-                        "sd2_attention_flat_workspace_bytes"):
+                        "sd2_attention_flat_workspace_bytes", "sd2_attention_prompt_workspace_bytes",
+                        "sd2_pages_fork_workspace_bytes", "sd2_pages_compact_workspace_bytes"):
             getattr(lib, name).restype = c_int32
     _LIB = lib
     return lib
@@ -421,3 +441,167 @@ def gemm(x: torch.Tensor, w: torch.Tensor, epilogue: int = 0, out: Optional[torc
                              0 if out is None else out.stride(0), _ptr(h), _ptr(bias), _ptr(seq),
                              0 if bias is None else bias.stride(0), impl, _stream(stream)))
     return h if epilogue in (2, 4) else out
+
+
+def _require(ok: bool, what: str):
+    """Refuse what the C ABI cannot see: a tensor's device, type, shape or strides."""
+    if not ok:
+        raise SD2Error(SD2_EINVAL, what)
+
+
+def _pool_shape(pool: torch.Tensor):
+    _require(pool.is_cuda and pool.dtype == torch.bfloat16 and pool.dim() == 6 and pool.is_contiguous() and
+             pool.shape[2] == 2 and pool.shape[4] == 16,
+             "pool must be a contiguous CUDA bf16 tensor [L, n_blocks, 2, Hkv, 16, hd]")
+    return pool.shape[0], pool.shape[1], pool.shape[3], pool.shape[5]
+
+
+def _ints(name: str, t: Optional[torch.Tensor], *shape, device):
+    """An optional contiguous int32 tensor on the pool's device, of this shape."""
+    _require(t is None or (t.dtype == torch.int32 and t.device == device and t.is_contiguous() and
+                           tuple(t.shape) == shape),
+             f"{name} must be a contiguous int32 tensor {list(shape)} on the pool's device")
+
+
+def _batch(table: torch.Tensor, cu_rows: torch.Tensor, kv_len: torch.Tensor, device):
+    _require(table.dim() == 2, "table must be int32 [n_seq, bt_stride]")
+    n, stride = table.shape
+    _ints("table", table, n, stride, device=device)
+    _ints("cu_rows", cu_rows, n + 1, device=device)
+    _ints("kv_len", kv_len, n, device=device)
+    return n, stride
+
+
+def _rows(name: str, t: torch.Tensor, dtypes, hd: int, device):
+    """Packed rows [M, heads, hd] whose heads are back to back; any row stride. Returns the stride."""
+    _require(t.dim() == 3 and t.dtype in dtypes and t.device == device and t.shape[2] == hd and t.shape[1] >= 1 and
+             (t.numel() == 0 or (t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == hd))),
+             f"{name} must be rows [M, heads, {hd}] on the pool's device, each row's heads back to back")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * hd
+
+
+def _workspace(given: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+    if given is None:
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+    _require(given.device == device and given.is_contiguous(), "workspace must be contiguous, on the pool's device")
+    return given
+
+
+def _used_on(stream, *tensors):
+    """Tensors allocated here for work on a stream that is not the current one: their memory may be reused
+    only after that work."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def attention_prompt(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, layer: int, cu_rows: torch.Tensor,
+                     kv_len: torch.Tensor, max_kv: Optional[int] = None, return_lse: bool = False,
+                     workspace: Optional[torch.Tensor] = None, err: Optional[torch.Tensor] = None, stream=None):
+    """Causal attention of packed prompt rows over the paged cache (sd2_attention_prompt). q bf16
+    [M, H, hd] (any row stride); pool bf16 [L, n_blocks, 2, Hkv, 16, hd]; table int32 [n_seq, bt_stride];
+    cu_rows int32 [n_seq + 1]; kv_len int32 [n_seq], the cached length with the new rows; max_kv a host
+    bound of it (default: the table's room). Returns bf16 [M, H * hd], with f32 [M, H] log-sum-exps if
+    `return_lse`. Rows of no sequence are left unwritten."""
+    lib = load_library()
+    L, n_blocks, Hkv, hd = _pool_shape(pool)
+    dev = pool.device
+    n_seq, stride = _batch(table, cu_rows, kv_len, dev)
+    ldq = _rows("q", q, (torch.bfloat16,), hd, dev)
+    _require(0 <= layer < L, "layer outside the pool")
+    M, H, _ = q.shape
+    max_kv = 16 * stride if max_kv is None else max(1, int(max_kv))
+    out = torch.empty((M, H * hd), dtype=torch.bfloat16, device=dev)
+    lse = torch.empty((M, H), dtype=torch.float32, device=dev) if return_lse else None
+    if M:
+        ws = _workspace(workspace, lib.sd2_attention_prompt_workspace_bytes(M, n_seq, H, Hkv, hd, max_kv), dev)
+        _check(lib, lib.sd2_attention_prompt(_ptr(q), ldq, M, H, Hkv, hd, _ptr(pool), n_blocks, _ptr(table), stride, layer,
+                                             _ptr(cu_rows), _ptr(kv_len), n_seq, max_kv, _ptr(out), _ptr(lse), _ptr(ws),
+                                             ws.numel() * ws.element_size(), _ptr(err), _stream(stream)))
+        _used_on(stream, out, lse, ws)
+    return (out, lse) if return_lse else out
+
+
+def pages_append(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, layer: int,
+                 cu_rows: torch.Tensor, kv_len: torch.Tensor, err: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Write packed K/V rows to their pages of one layer (sd2_pages_append). k, v [M, Hkv, hd], f32 or
+    bf16, any row stride (views of a fused projection's output will do); the batch as in
+    attention_prompt."""
+    lib = load_library()
+    L, n_blocks, Hkv, hd = _pool_shape(pool)
+    dev = pool.device
+    n_seq, stride = _batch(table, cu_rows, kv_len, dev)
+    _require(0 <= layer < L, "layer outside the pool")
+    _require(k.shape == v.shape and k.dtype == v.dtype and k.dim() == 3 and k.shape[1] == Hkv,
+             "k and v must have one type and the shape [M, Hkv, hd]")
+    ldk = _rows("k", k, (torch.float32, torch.bfloat16), hd, dev)
+    ldv = _rows("v", v, (torch.float32, torch.bfloat16), hd, dev)
+    if k.shape[0]:
+        _check(lib, lib.sd2_pages_append(_ptr(k), ldk, _ptr(v), ldv, DTYPE_BF16 if k.dtype == torch.bfloat16 else DTYPE_F32,
+                                         k.shape[0], Hkv, hd, _ptr(pool), n_blocks, _ptr(table), stride, layer,
+                                         _ptr(cu_rows), _ptr(kv_len), n_seq, _ptr(err), _stream(stream)))
+
+
+class ForkedPages(NamedTuple):
+    table: torch.Tensor    # int32 [n_out, bt_stride]
+    length: torch.Tensor   # int32 [n_out]
+    pages: torch.Tensor    # int32 [n_out]: pages held
+    ref: torch.Tensor      # int32 [n_blocks]: holders of each page
+
+
+def pages_fork(pool: torch.Tensor, table: torch.Tensor, length: torch.Tensor, parent: torch.Tensor,
+               keep: Optional[torch.Tensor] = None, grow: Optional[torch.Tensor] = None,
+               pinned: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               err: Optional[torch.Tensor] = None, stream=None) -> ForkedPages:
+    """A new batch out of an old one (sd2_pages_fork): sequence b continues old sequence parent[b] (-1:
+    none) after its first keep[b] positions, with room for grow[b] more. Sequences that no parent entry
+    names give up their pages; whole pages are shared, shared tails copied."""
+    lib = load_library()
+    L, n_blocks, Hkv, hd = _pool_shape(pool)
+    dev = pool.device
+    _require(table.dim() == 2 and parent.dim() == 1 and parent.numel() > 0, "table must be 2-D and parent 1-D, not empty")
+    (n_seq, stride), n = table.shape, parent.numel()
+    _ints("table", table, n_seq, stride, device=dev)
+    _ints("length", length, n_seq, device=dev)
+    for name, t in (("parent", parent), ("keep", keep), ("grow", grow)):
+        _ints(name, t, n, device=dev)
+    _ints("pinned", pinned, n_blocks, device=dev)
+    f = ForkedPages(torch.empty((n, stride), dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev),
+                    torch.empty(n, dtype=torch.int32, device=dev), torch.empty(n_blocks, dtype=torch.int32, device=dev))
+    ws = _workspace(workspace, lib.sd2_pages_fork_workspace_bytes(n, n_blocks), dev)
+    _check(lib, lib.sd2_pages_fork(_ptr(pool), L, n_blocks, Hkv, hd, _ptr(table), stride, _ptr(length), n_seq, _ptr(parent),
+                                   _ptr(keep), _ptr(grow), _ptr(pinned), n, _ptr(f.table), _ptr(f.length), _ptr(f.pages),
+                                   _ptr(f.ref), _ptr(ws), ws.numel() * ws.element_size(), _ptr(err), _stream(stream)))
+    _used_on(stream, *f, ws)
+    return f
+
+
+class CompactedPages(NamedTuple):
+    table: torch.Tensor    # int32 [n_seq, bt_stride]
+    ref: torch.Tensor      # int32 [n_blocks]
+    map: torch.Tensor      # int32 [n_blocks]: a page's new id, -1 for a free one
+    n_live: torch.Tensor   # int32 [1]
+
+
+def pages_compact(pool: torch.Tensor, table: torch.Tensor, pages: torch.Tensor, ref: torch.Tensor,
+                  workspace: Optional[torch.Tensor] = None, err: Optional[torch.Tensor] = None,
+                  stream=None) -> CompactedPages:
+    """Move the pool's live pages (ref > 0) to the lowest ids (sd2_pages_compact); `pages` [n_seq] are the
+    entries in use of each table row."""
+    lib = load_library()
+    L, n_blocks, Hkv, hd = _pool_shape(pool)
+    dev = pool.device
+    _require(table.dim() == 2, "table must be int32 [n_seq, bt_stride]")
+    n_seq, stride = table.shape
+    _ints("table", table, n_seq, stride, device=dev)
+    _ints("pages", pages, n_seq, device=dev)
+    _ints("ref", ref, n_blocks, device=dev)
+    c = CompactedPages(torch.empty_like(table), torch.empty_like(ref), torch.empty_like(ref),
+                       torch.empty(1, dtype=torch.int32, device=dev))
+    ws = _workspace(workspace, lib.sd2_pages_compact_workspace_bytes(n_blocks), dev)
+    _check(lib, lib.sd2_pages_compact(_ptr(pool), L, n_blocks, Hkv, hd, _ptr(table), stride, _ptr(pages), n_seq, _ptr(ref),
+                                      _ptr(c.table), _ptr(c.ref), _ptr(c.map), _ptr(c.n_live), _ptr(ws),
+                                      ws.numel() * ws.element_size(), _ptr(err), _stream(stream)))
+    _used_on(stream, *c, ws)
+    return c

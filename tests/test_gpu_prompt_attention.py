@@ -1,0 +1,283 @@
+"""Prompt attention over the paged cache (sd2_attention_prompt) against its definition in 64 bits.
+
+The bound of every output is derived from the arithmetic: probabilities are rounded to bf16 before the
+second product (relative 2^-9 each), the result once more to bf16 (2^-9), everything else is 32-bit;
+so |out - o| <= 2^-9 (sum_j p_j |v_j| + |o|), with a quarter on top for the 32-bit terms (scores of at
+most a few tens carry less than 1e-4 of relative error into a probability). Log-sum-exps carry only the
+scores' 32-bit error: at most hd * 2^-23 * sum_i |q_i k_i| / sqrt(hd), below 4e-4 for the inputs here.
+Pages no row may see, and the rows of a last page beyond the cached length, hold NaN.
+"""
+import pytest
+import torch
+
+from paper_2511_09844_gb300 import sd2
+
+pytestmark = pytest.mark.gpu
+
+ERR_RANGE = 4
+LSE_TOL = 4e-4
+
+
+def _case(rows, kv, H, Hkv, hd, seed=0, layers=2, layer=1, slack=2, scale=1.5):
+    """Packed queries and a pool whose visible rows are random, everything else NaN."""
+    g = torch.Generator().manual_seed(seed)
+    n = len(rows)
+    pages = [(x + 15) // 16 for x in kv]
+    stride = max(1, max(pages)) + slack
+    n_blocks = sum(pages) + 5
+    ids = torch.randperm(n_blocks, generator=g)[: sum(pages)].tolist()
+    pool = torch.full((layers, n_blocks, 2, Hkv, 16, hd), float("nan"), dtype=torch.bfloat16)
+    table = torch.zeros(n, stride, dtype=torch.int32)
+    at = 0
+    for s in range(n):
+        for i in range(pages[s]):
+            p, fill = ids[at], min(16, kv[s] - 16 * i)
+            table[s, i] = p
+            pool[layer, p, :, :, :fill] = torch.randn(2, Hkv, fill, hd, generator=g).to(torch.bfloat16)
+            at += 1
+    cu = torch.tensor([0] + rows).cumsum(0).to(torch.int32)
+    q = (torch.randn(sum(rows), H, hd, generator=g) * scale).to(torch.bfloat16)
+    return dict(q=q, pool=pool, table=table, cu=cu, kv_len=torch.tensor(kv, dtype=torch.int32), rows=rows, kv=kv,
+                layer=layer, H=H, Hkv=Hkv, hd=hd)
+
+
+def _definition(c):
+    """(out, lse, sum_j p_j |v_j|) in float64."""
+    H, Hkv, hd = c["H"], c["Hkv"], c["hd"]
+    M = c["q"].shape[0]
+    out, mag = torch.zeros(M, H, hd, dtype=torch.float64), torch.zeros(M, H, hd, dtype=torch.float64)
+    lse = torch.full((M, H), float("-inf"), dtype=torch.float64)
+    for s, (n, L) in enumerate(zip(c["rows"], c["kv"])):
+        if n == 0 or L == 0:
+            continue
+        kv = c["pool"][c["layer"], c["table"][s, : (L + 15) // 16].long()].double()
+        k = kv[:, 0].transpose(0, 1).reshape(Hkv, -1, hd)[:, :L].repeat_interleave(H // Hkv, 0)
+        v = kv[:, 1].transpose(0, 1).reshape(Hkv, -1, hd)[:, :L].repeat_interleave(H // Hkv, 0)
+        r0 = int(c["cu"][s])
+        z = torch.einsum("rhd,hkd->hrk", c["q"][r0:r0 + n].double(), k) / hd ** 0.5
+        p = torch.arange(L - n, L)
+        z.masked_fill_(torch.arange(L)[None, :] > p[:, None], float("-inf"))
+        seen = p >= 0
+        zs = z[:, seen]
+        lse[r0:r0 + n][seen] = torch.logsumexp(zs, -1).T
+        w = torch.softmax(zs, -1)
+        out[r0:r0 + n][seen] = torch.einsum("hrk,hkd->rhd", w, v)
+        mag[r0:r0 + n][seen] = torch.einsum("hrk,hkd->rhd", w, v.abs())
+    return out.reshape(M, -1), lse, mag.reshape(M, -1)
+
+
+def _run(c, max_kv=None, **kw):
+    d = {k: v.cuda() for k, v in c.items() if isinstance(v, torch.Tensor)}
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = sd2.attention_prompt(d["q"], d["pool"], d["table"], c["layer"], d["cu"], d["kv_len"],
+                                    max_kv=max(c["kv"]) if max_kv is None else max_kv, return_lse=True, err=err, **kw)
+    torch.cuda.synchronize()
+    return out.cpu(), lse.cpu(), int(err.item())
+
+
+def _check(c, out, lse, want=None):
+    o, l, mag = want or _definition(c)
+    off = (out.double() - o).abs() - 1.25 * 2 ** -9 * (mag + o.abs())
+    assert torch.isfinite(out).all()
+    assert off.max().item() <= 1e-6, off.max().item()
+    empty = torch.isinf(l)
+    assert torch.equal(torch.isinf(lse) & (lse < 0), empty)
+    assert (lse.double() - l)[~empty].abs().max().item() <= LSE_TOL if (~empty).any() else True
+    assert (out.view(l.shape[0], l.shape[1], -1)[empty] == 0).all()
+
+
+HEADS = [(4, 4, 64), (2, 2, 64), (14, 2, 64), (8, 2, 64), (8, 2, 128), (10, 2, 128), (3, 1, 128)]
+
+
+@pytest.mark.parametrize("H,Hkv,hd", HEADS)
+@pytest.mark.parametrize("rows,prefix", [
+    ([1], [0]), ([37], [0]), ([128], [0]), ([129], [0]), ([300, 1, 64, 17], [0, 0, 0, 0]),
+    ([1], [15]), ([1], [16]), ([5, 40], [1000, 3]), ([257, 6], [130, 777])])
+def test_against_the_definition(H, Hkv, hd, rows, prefix):
+    c = _case(rows, [a + b for a, b in zip(rows, prefix)], H, Hkv, hd, seed=len(rows) + H)
+    out, lse, err = _run(c)
+    assert err == 0
+    _check(c, out, lse)
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(32, 1, 64), (65, 1, 64), (96, 1, 128), (128, 1, 64), (128, 1, 128), (24, 2, 128)])
+def test_many_heads_per_kv_head(H, Hkv, hd):
+    c = _case([3, 21], [3, 200], H, Hkv, hd, seed=H)
+    out, lse, err = _run(c)
+    assert err == 0
+    _check(c, out, lse)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_rows_that_see_nothing_and_empty_sequences(hd):
+    """More new rows than cached positions leave the first rows nothing; sequences of no rows, of no cache."""
+    c = _case([0, 20, 5, 0, 3, 0], [0, 7, 0, 40, 3, 0], 8, 2, hd, seed=5)
+    out, lse, err = _run(c, max_kv=40)
+    assert err == 0
+    _check(c, out, lse)
+    assert torch.isinf(lse[:13]).all() and torch.isfinite(lse[13:20]).all() and torch.isinf(lse[20:25]).all()
+
+
+@pytest.mark.parametrize("rows,prefix", [([1], [5000]), ([6, 17], [20000, 9001]), ([2, 1, 9], [4095, 4096, 100]),
+                                         ([33, 1], [3333, 0])])
+@pytest.mark.parametrize("H,Hkv,hd", [(8, 2, 128), (14, 2, 64)])
+@pytest.mark.parametrize("claim", ["exact", "short", "long"])
+def test_few_rows_on_long_caches(rows, prefix, H, Hkv, hd, claim):
+    """Few rows: the cache is cut into splits that are joined. max_kv only sizes the split."""
+    kv = [a + b for a, b in zip(rows, prefix)]
+    c = _case(rows, kv, H, Hkv, hd, seed=7)
+    out, lse, err = _run(c, max_kv={"exact": max(kv), "short": 64, "long": 1 << 20}[claim])
+    assert err == 0
+    _check(c, out, lse)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_large_scores_and_growing_maxima(hd):
+    """Peaked softmaxes whose running maximum grows along the cache by far more than a tile's spread."""
+    c = _case([200], [700], 4, 2, hd, seed=11, scale=1.0)
+    ramp = torch.linspace(0.05, 6.0, 700)
+    layer, table = c["layer"], c["table"]
+    for j in range(700):
+        c["pool"][layer, table[0, j // 16].long(), 0, :, j % 16] *= ramp[j]
+    out, lse, err = _run(c)
+    o, l, mag = _definition(c)
+    assert err == 0
+    # scores to about 60: their 32-bit error, hd * 2^-23 * sum |q k| / sqrt(hd), is up to 4 times that of the others
+    off = (out.double() - o).abs() - 1.25 * 2 ** -9 * (mag + o.abs()) - 2e-3 * mag
+    assert off.max().item() <= 1e-6
+    assert (lse.double() - l).abs().max().item() <= 4 * LSE_TOL
+
+
+def test_infinite_scores_weigh_one_position():
+    """A key that wins by more than 32 bits can express: its value alone, exactly."""
+    c = _case([40], [200], 4, 2, 64, seed=12)
+    c["q"][:] = 1.0
+    c["pool"][c["layer"], c["table"][0, 3].long(), 0, :, 5] = 1000.0     # position 53
+    out, lse, err = _run(c)
+    v = c["pool"][c["layer"], c["table"][0, 3].long(), 1, :, 5]
+    assert err == 0 and torch.equal(out.view(40, 2, 2, 64), v[None, :, None].expand(40, 2, 2, 64))
+
+
+def test_strided_queries_other_streams_and_repeats():
+    """Queries cut out of a fused projection's rows, on a side stream with a caller's workspace: the bits of
+    the plain call, every time."""
+    c = _case([70, 129, 3], [70, 500, 2003], 8, 2, 128, seed=13)
+    out, lse, _ = _run(c)
+    _check(c, out, lse)
+    d = {k: v.cuda() for k, v in c.items() if isinstance(v, torch.Tensor)}
+    fused = torch.full((c["q"].shape[0], 12, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    fused[:, 2:10] = d["q"]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    need = sd2.load_library().sd2_attention_prompt_workspace_bytes(fused.shape[0], 3, 8, 2, 128, 2003)
+    ws = torch.full((need,), 0xAB, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        o2, l2 = sd2.attention_prompt(fused[:, 2:10], d["pool"], d["table"], c["layer"], d["cu"], d["kv_len"], max_kv=2003,
+                                      return_lse=True, workspace=ws, stream=side)
+        side.synchronize()
+        assert torch.equal(o2.cpu(), out) and torch.equal(l2.cpu(), lse)
+
+
+def test_table_without_room_and_rows_of_no_sequence():
+    """A length beyond the table's room is read to its end; rows after the last sequence are not written."""
+    c = _case([4], [64], 4, 2, 64, seed=14, slack=0)
+    out, lse, err = _run(c)
+    _check(c, out, lse)
+    d = {k: v.cuda() for k, v in c.items() if isinstance(v, torch.Tensor)}
+    longer = d["kv_len"] + 36                       # rows at 96 .. 99, positions 64 .. 99 have no page
+    o2 = sd2.attention_prompt(d["q"], d["pool"], d["table"], c["layer"], d["cu"], longer, max_kv=100)
+    every = dict(c, q=c["q"])
+    z = _definition(dict(every, rows=[4], kv=[64]))[0]
+    k = c["pool"][c["layer"], c["table"][0].long()].double()
+    kk = k[:, 0].transpose(0, 1).reshape(2, 64, 64).repeat_interleave(2, 0)
+    vv = k[:, 1].transpose(0, 1).reshape(2, 64, 64).repeat_interleave(2, 0)
+    w = torch.softmax(torch.einsum("rhd,hkd->hrk", c["q"].double(), kk) / 8, -1)
+    o, mag = torch.einsum("hrk,hkd->rhd", w, vv), torch.einsum("hrk,hkd->rhd", w, vv.abs())
+    assert z.shape == o.reshape(4, -1).shape
+    assert ((o2.cpu().double().view_as(o) - o).abs() - 1.25 * 2 ** -9 * (mag + o.abs())).max().item() <= 1e-6
+    # three extra packed rows beyond cu_rows[n_seq]
+    lib = sd2.load_library()
+    q = torch.cat([d["q"], d["q"][:3]])
+    guard = torch.full((7, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(lib.sd2_attention_prompt_workspace_bytes(7, 1, 4, 2, 64, 64), dtype=torch.uint8, device="cuda")
+    st = lib.sd2_attention_prompt(sd2._ptr(q), 256, 7, 4, 2, 64, sd2._ptr(d["pool"]), d["pool"].shape[1],
+                                  sd2._ptr(d["table"]), d["table"].shape[1], c["layer"], sd2._ptr(d["cu"]),
+                                  sd2._ptr(d["kv_len"]), 1, 64, sd2._ptr(guard), None, sd2._ptr(ws), ws.numel(), None,
+                                  sd2._stream())
+    torch.cuda.synchronize()
+    assert st == 0 and torch.equal(guard[:4].cpu(), out) and (guard[4:] == 7.0).all()
+
+
+def test_bad_page_ids_are_reported():
+    c = _case([5, 6], [50, 60], 4, 2, 64, seed=15)
+    want = _definition(c)
+    for bad in (-1, c["pool"].shape[1], 2 ** 31 - 1, -2 ** 31):
+        t = dict(c, table=c["table"].clone())
+        t["table"][0, 1] = bad
+        out, lse, err = _run(t)
+        assert err == ERR_RANGE
+        sub = lambda x: x[5:]  # noqa: E731
+        off = (sub(out).double() - sub(want[0])).abs() - 1.25 * 2 ** -9 * (sub(want[2]) + sub(want[0]).abs())
+        assert off.max().item() <= 1e-6
+
+
+def test_a_cache_beyond_32_bit_offsets():
+    """The last pages of a layer whose pool offsets pass 2^31 elements (a 4.5 GB pool, one layer of 2)."""
+    Hkv, hd = 8, 128
+    n_blocks = 36000                                  # 2 layers x 36000 x 32768 elements
+    pool = torch.zeros(2, n_blocks, 2, Hkv, 16, hd, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator().manual_seed(16)
+    small = _case([20], [100], 16, Hkv, hd, seed=16)
+    ids = torch.arange(n_blocks - 7, n_blocks, dtype=torch.int32)
+    pool[1, ids.long()] = small["pool"][1, small["table"][0, :7].long()].cuda()
+    table = ids.view(1, 7).contiguous()
+    assert g is not None
+    out, lse = sd2.attention_prompt(small["q"].cuda(), pool, table.cuda(), 1, small["cu"].cuda(), small["kv_len"].cuda(),
+                                    max_kv=100, return_lse=True)
+    _check(small, out.cpu(), lse.cpu())
+
+
+def test_tokens_one_at_a_time_agree_with_the_whole_prompt():
+    """Each row alone (its own call, as in decoding) against the packed call: the same definition."""
+    c = _case([30], [90], 8, 2, 128, seed=17)
+    want = _definition(c)
+    d = {k: v.cuda() for k, v in c.items() if isinstance(v, torch.Tensor)}
+    one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    outs, lses = [], []
+    for i in range(30):
+        o, l = sd2.attention_prompt(d["q"][i:i + 1], d["pool"], d["table"], c["layer"], one, d["kv_len"] - 29 + i,
+                                    max_kv=90, return_lse=True)
+        outs.append(o.cpu())
+        lses.append(l.cpu())
+    _check(c, torch.cat(outs), torch.cat(lses), want)
+
+
+def test_agrees_with_decode_attention():
+    """The rows of a verification block through both attention kernels of the library."""
+    c = _case([6, 6], [500, 131], 32, 8, 128, seed=18)
+    c["pool"].nan_to_num_(0.0)                        # decode attention wants finite pages
+    out, lse, _ = _run(c)
+    d = {k: v.cuda() for k, v in c.items() if isinstance(v, torch.Tensor)}
+    i = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    pos = i(list(range(494, 500)) + list(range(125, 131)))
+    dec = sd2.attention(d["q"].float(), d["pool"], d["table"], c["layer"], pos, i([0, 6]), i([6, 6]), i([0, 1]), 6, 4, 128)
+    o, l, mag = _definition(c)
+    # both round probabilities and results to bf16
+    assert ((dec.cpu().double() - out.double()).abs() - 2.5 * 2 ** -9 * (mag + o.abs())).max().item() <= 1e-6
+
+
+def test_refusals_of_device_tensors():
+    """What the binding refuses of tensors on the GPU: types, shapes, strides, layers."""
+    c = _case([4], [20], 4, 2, 64, seed=19)
+    d = {k: v.cuda() for k, v in c.items() if isinstance(v, torch.Tensor)}
+    ok = dict(q=d["q"], pool=d["pool"], table=d["table"], layer=1, cu_rows=d["cu"], kv_len=d["kv_len"], max_kv=20)
+    sd2.attention_prompt(**ok)
+    for bad in (dict(q=d["q"].float()), dict(q=d["q"].transpose(0, 1)), dict(q=d["q"][:, :3]), dict(q=d["q"][..., :32]),
+                dict(q=d["q"][:1].expand(4, 4, 64)), dict(pool=d["pool"][:, ::2]), dict(pool=d["pool"].float()),
+                dict(pool=d["pool"][0]), dict(table=d["table"].long()), dict(table=d["table"].T), dict(layer=2),
+                dict(layer=-1), dict(cu_rows=d["cu"][:1]), dict(kv_len=d["kv_len"].float()), dict(kv_len=d["kv_len"].cpu()),
+                dict(workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(sd2.SD2Error, match="EINVAL"):
+            sd2.attention_prompt(**dict(ok, **bad))
+    assert sd2.attention_prompt(**dict(ok, q=d["q"][:0], cu_rows=d["cu"] * 0)).shape == (0, 256)

@@ -1,0 +1,119 @@
+"""Refusals of the shared-cache entry points (prompt attention, append, fork, compact): bad arguments end
+in SD2_EINVAL with a reason before any device work, and no call falls back to anything else."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2511_09844_gb300 import build, sd2
+
+P = ctypes.c_void_p(1 << 20)          # stand-in addresses: every call fails a host check before using them
+Q = ctypes.c_void_p(1 << 21)
+U = ctypes.c_void_p((1 << 20) + 4)
+
+
+@pytest.fixture(scope="module")
+def L():
+    build.build()
+    return sd2.load_library()
+
+
+def refused(L, st, word):
+    return st == sd2.SD2_EINVAL and word in L.sd2_last_error(None)
+
+
+def test_prompt_attention_refuses(L):
+    assert L.sd2_attention_prompt_workspace_bytes(0, 1, 8, 2, 64, 10) == 0
+    assert L.sd2_attention_prompt_workspace_bytes(5, 1, 8, 3, 64, 10) == 0
+    need = L.sd2_attention_prompt_workspace_bytes(7, 2, 32, 8, 128, 65536)
+    assert need > 0 and need % 256 == 0
+
+    def call(q=P, ldq=4096, M=7, H=32, Hkv=8, hd=128, pool=P, nb=64, table=P, stride=8, layer=0, cu=P, kv=P, n_seq=2,
+             max_kv=65536, out=P, work=P, nbytes=need):
+        return L.sd2_attention_prompt(q, ldq, M, H, Hkv, hd, pool, nb, table, stride, layer, cu, kv, n_seq, max_kv, out, None,
+                                      work, nbytes, None, None)
+    for name in ("q", "pool", "table", "cu", "kv", "out", "work"):
+        assert refused(L, call(**{name: None}), b"null"), name
+    for kw in (dict(hd=96), dict(H=30), dict(H=129 * 8, ldq=129 * 8 * 128), dict(Hkv=0), dict(M=-1)):
+        assert refused(L, call(**kw), b"bad attention shape"), kw
+    for kw in (dict(nb=0), dict(stride=0), dict(n_seq=0), dict(layer=-1), dict(max_kv=0), dict(stride=(1 << 26) + 1)):
+        assert refused(L, call(**kw), b"need n_blocks"), kw
+    assert refused(L, call(nb=1 << 28), b"31 bits")
+    for kw in (dict(ldq=4088), dict(ldq=4100), dict(q=U), dict(pool=U), dict(out=U)):
+        assert refused(L, call(**kw), b"16-byte"), kw
+    assert refused(L, call(nbytes=need - 1), b"workspace too small")
+    assert refused(L, call(work=U), b"256-byte")
+    assert call(M=0) == sd2.SD2_OK
+
+
+def test_append_refuses(L):
+    def call(k=P, ldk=1024, v=P, ldv=1024, dtype=sd2.DTYPE_BF16, M=7, Hkv=8, hd=128, pool=P, nb=64, table=P, stride=8,
+             layer=0, cu=P, kv=P, n_seq=2):
+        return L.sd2_pages_append(k, ldk, v, ldv, dtype, M, Hkv, hd, pool, nb, table, stride, layer, cu, kv, n_seq, None, None)
+    for name in ("k", "v", "pool", "table", "cu", "kv"):
+        assert refused(L, call(**{name: None}), b"null"), name
+    assert refused(L, call(dtype=2), b"dtype")
+    for kw in (dict(M=-1), dict(stride=0), dict(n_seq=0), dict(layer=-1)):
+        assert refused(L, call(**kw), b"need M"), kw
+    for kw in (dict(nb=0), dict(Hkv=0), dict(hd=12), dict(hd=0)):
+        assert refused(L, call(**kw), b"need L"), kw
+    assert refused(L, call(pool=U), b"pool not 16-byte")
+    for kw in (dict(ldk=1016), dict(ldv=1028), dict(k=U), dict(v=U)):
+        assert refused(L, call(**kw), b"rows of k and v"), kw
+    assert call(M=0) == sd2.SD2_OK
+
+
+def test_fork_refuses(L):
+    assert L.sd2_pages_fork_workspace_bytes(0, 9) == 0 and L.sd2_pages_fork_workspace_bytes(9, 0) == 0
+    need = L.sd2_pages_fork_workspace_bytes(4, 64)
+    assert need % 256 == 0 and need >= 4 * 16 + 64 * 12
+
+    def call(pool=P, layers=2, nb=64, Hkv=8, hd=128, table=P, stride=8, ln=P, n_seq=2, parent=P, n_out=4, t2=Q, l2=Q, p2=Q,
+             r2=Q, work=P, nbytes=need, pinned=None):
+        return L.sd2_pages_fork(pool, layers, nb, Hkv, hd, table, stride, ln, n_seq, parent, None, None, pinned, n_out, t2, l2,
+                                p2, r2, work, nbytes, None, None)
+    for name in ("pool", "table", "ln", "parent", "t2", "l2", "p2", "r2", "work"):
+        assert refused(L, call(**{name: None}), b"null"), name
+    for kw in (dict(layers=0), dict(nb=0), dict(hd=4)):
+        assert refused(L, call(**kw), b"need L"), kw
+    assert refused(L, call(layers=1 << 30), b"page too large")
+    for kw in (dict(n_seq=0), dict(n_out=0), dict(stride=0)):
+        assert refused(L, call(**kw), b"need n_seq"), kw
+    for kw in (dict(t2=P), dict(l2=P), dict(pinned=Q)):
+        assert refused(L, call(**kw), b"outputs must not"), kw
+    assert refused(L, call(nbytes=need - 1), b"workspace too small")
+    assert refused(L, call(work=U), b"256-byte")
+
+
+def test_compact_refuses(L):
+    assert L.sd2_pages_compact_workspace_bytes(0) == 0
+    need = L.sd2_pages_compact_workspace_bytes(64)
+    assert need % 256 == 0 and need >= 64 * 12
+
+    def call(pool=P, layers=2, nb=64, Hkv=8, hd=128, table=P, stride=8, pages=P, n_seq=2, ref=P, t2=Q, r2=Q, m2=Q, n2=Q,
+             work=P, nbytes=need):
+        return L.sd2_pages_compact(pool, layers, nb, Hkv, hd, table, stride, pages, n_seq, ref, t2, r2, m2, n2, work, nbytes,
+                                   None, None)
+    for name in ("pool", "table", "pages", "ref", "t2", "r2", "m2", "n2", "work"):
+        assert refused(L, call(**{name: None}), b"null"), name
+    assert refused(L, call(layers=0), b"need L")
+    for kw in (dict(n_seq=0), dict(stride=0)):
+        assert refused(L, call(**kw), b"need n_seq"), kw
+    assert refused(L, call(r2=P), b"outputs must not")
+    assert refused(L, call(nbytes=need - 1), b"workspace too small")
+    assert refused(L, call(work=U), b"256-byte")
+
+
+def test_binding_refuses_other_tensors(L):
+    """Tensors the C ABI cannot judge: host memory is refused, not computed some other way."""
+    pool = torch.zeros(1, 4, 2, 2, 16, 64, dtype=torch.bfloat16)
+    i = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    q = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
+    kv = torch.zeros(3, 2, 64)
+    table = torch.zeros(1, 2, dtype=torch.int32)
+    for call in (lambda: sd2.attention_prompt(q, pool, table, 0, i(0, 3), i(3)),
+                 lambda: sd2.pages_append(kv, kv, pool, table, 0, i(0, 3), i(3)),
+                 lambda: sd2.pages_fork(pool, table, i(3), i(0)),
+                 lambda: sd2.pages_compact(pool, table, i(1), i(1, 0, 0, 0))):
+        with pytest.raises(sd2.SD2Error, match="EINVAL.*pool must be"):
+            call()
