@@ -1,9 +1,10 @@
 """Prompt attention over the paged cache (sd2_attention_prompt) against its definition in 64 bits.
 
 The bound of every output is derived from the arithmetic: probabilities are rounded to bf16 before the
-second product (relative 2^-9 each), the result once more to bf16 (2^-9), everything else is 32-bit;
-so |out - o| <= 2^-9 (sum_j p_j |v_j| + |o|), with a quarter on top for the 32-bit terms (scores of at
-most a few tens carry less than 1e-4 of relative error into a probability). Log-sum-exps carry only the
+second product and the result once more, each by at most a relative 2^-8 (8 significant bits: half of
+the spacing 2^-7), everything else is 32-bit; so |out - o| <= 2^-8 (sum_j p_j |v_j| + |o|), with
+2e-4 sum_j p_j |v_j| on top for the 32-bit terms (scores of at most a few tens carry about 1e-4 of
+relative error into a probability). Log-sum-exps carry only the
 scores' 32-bit error: at most hd * 2^-23 * sum_i |q_i k_i| / sqrt(hd), below 4e-4 for the inputs here.
 Pages no row may see, and the rows of a last page beyond the cached length, hold NaN.
 """
@@ -66,6 +67,10 @@ def _definition(c):
     return out.reshape(M, -1), lse, mag.reshape(M, -1)
 
 
+def _bound(o, mag):
+    return 2 ** -8 * (mag + o.abs()) + 2e-4 * mag
+
+
 def _run(c, max_kv=None, **kw):
     d = {k: v.cuda() for k, v in c.items() if isinstance(v, torch.Tensor)}
     err = torch.zeros(1, dtype=torch.int32, device="cuda")
@@ -77,7 +82,7 @@ def _run(c, max_kv=None, **kw):
 
 def _check(c, out, lse, want=None):
     o, l, mag = want or _definition(c)
-    off = (out.double() - o).abs() - 1.25 * 2 ** -9 * (mag + o.abs())
+    off = (out.double() - o).abs() - _bound(o, mag)
     assert torch.isfinite(out).all()
     assert off.max().item() <= 1e-6, off.max().item()
     empty = torch.isinf(l)
@@ -143,7 +148,7 @@ def test_large_scores_and_growing_maxima(hd):
     o, l, mag = _definition(c)
     assert err == 0
     # scores to about 60: their 32-bit error, hd * 2^-23 * sum |q k| / sqrt(hd), is up to 4 times that of the others
-    off = (out.double() - o).abs() - 1.25 * 2 ** -9 * (mag + o.abs()) - 2e-3 * mag
+    off = (out.double() - o).abs() - _bound(o, mag) - 2e-3 * mag
     assert off.max().item() <= 1e-6
     assert (lse.double() - l).abs().max().item() <= 4 * LSE_TOL
 
@@ -195,7 +200,7 @@ def test_table_without_room_and_rows_of_no_sequence():
     w = torch.softmax(torch.einsum("rhd,hkd->hrk", c["q"].double(), kk) / 8, -1)
     o, mag = torch.einsum("hrk,hkd->rhd", w, vv), torch.einsum("hrk,hkd->rhd", w, vv.abs())
     assert z.shape == o.reshape(4, -1).shape
-    assert ((o2.cpu().double().view_as(o) - o).abs() - 1.25 * 2 ** -9 * (mag + o.abs())).max().item() <= 1e-6
+    assert ((o2.cpu().double().view_as(o) - o).abs() - _bound(o, mag)).max().item() <= 1e-6
     # three extra packed rows beyond cu_rows[n_seq]
     lib = sd2.load_library()
     q = torch.cat([d["q"], d["q"][:3]])
@@ -218,7 +223,7 @@ def test_bad_page_ids_are_reported():
         out, lse, err = _run(t)
         assert err == ERR_RANGE
         sub = lambda x: x[5:]  # noqa: E731
-        off = (sub(out).double() - sub(want[0])).abs() - 1.25 * 2 ** -9 * (sub(want[2]) + sub(want[0]).abs())
+        off = (sub(out).double() - sub(want[0])).abs() - _bound(sub(want[0]), sub(want[2]))
         assert off.max().item() <= 1e-6
 
 
@@ -264,7 +269,7 @@ def test_agrees_with_decode_attention():
     dec = sd2.attention(d["q"].float(), d["pool"], d["table"], c["layer"], pos, i([0, 6]), i([6, 6]), i([0, 1]), 6, 4, 128)
     o, l, mag = _definition(c)
     # both round probabilities and results to bf16
-    assert ((dec.cpu().double() - out.double()).abs() - 2.5 * 2 ** -9 * (mag + o.abs())).max().item() <= 1e-6
+    assert ((dec.cpu().double() - out.double()).abs() - 2 * _bound(o, mag)).max().item() <= 1e-6
 
 
 def test_refusals_of_device_tensors():
