@@ -1,92 +1,514 @@
 // Attention of packed prompt rows over the paged KV cache: causal, grouped heads, sequences of
 // different lengths, each with or without positions that were cached before.
+//
+// For a row at position p: o = sum_{j<=p} e^{z_j - m} v_j / sum_{j<=p} e^{z_j - m}, z_j = q . k_j / sqrt(hd).
+// The positions are walked once in tiles of 128, with the running maximum m and sum l of each row in
+// registers (the sums, the scores and the accumulated o in fp32; probabilities are rounded to bf16 for the
+// second product, whose operands the tensor cores take in 16 bits).
+//
+// One CTA takes two query tiles ("slots") of 128 query vectors each: T = 128 / G tokens of one sequence,
+// all G heads that share the KV head, so that every K/V tile fetched serves 256 query vectors. Roles:
+//   warps 0-3, 4-7  softmax of slot 0, 1: one thread per query vector (the 128 TMEM lanes); scores come
+//                   from TMEM, probabilities go back over them as bf16
+//   warp 8          TMA loads: Q once, then K and V tiles of 8 pages (a box per page and 64 columns,
+//                   128-byte swizzle) through a ring
+//   warp 9          the MMAs: S = Q K^T from shared memory, O += P V with P in TMEM and V as the
+//                   [position][hd] tile that it is (MN-major); while one slot is in its softmax the
+//                   other's products run
+// TMEM: S0, S1 (P over them), O0, O1. O is rescaled in TMEM by the softmax threads, and only when a row's
+// maximum has grown by more than 2^8 since the last time: until then probabilities are taken relative to
+// the older maximum, which changes no rounding (bf16 and fp32 are relative) and cannot overflow.
+//
+// Bound: the tensor cores for long prompts (4 hd flops per visible pair and head), HBM for few rows on a
+// long cache. Few rows leave SMs idle, so the positions are then cut over gridDim.z splits that a second
+// kernel joins.
 #include "sd2.h"
-#include "common.cuh"
 #include "kernels.h"
+#include "tc.cuh"
 
+#include <algorithm>
 #include <string>
 
 namespace sd2 {
 void record_last_error(const std::string& m);  // engine.cu
 
 namespace {
+using namespace tc;
 
 constexpr int kPage = 16;
+constexpr int kTile = 128;                 // positions per K/V tile, query vectors per slot
+constexpr int kThreads = 320;
+constexpr int kMaxStages = 8;
+constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum that makes O be rescaled
 
 struct PromptArgs {
-  const bf16* q;
-  long long ldq;
-  int M, H, Hkv;
-  const bf16* pool;            // the layer's pages
-  int n_blocks;
-  const int* table;
-  int bt_stride;
-  const int *cu, *kv_len;
-  int n_seq;
+  CUtensorMap map_q, map_kv;
+  int M, H, Hkv, G, T;                     // G heads per KV head, T tokens per slot
+  int n_blocks, bt_stride, n_seq, n_splits;
+  int kv_rows;                             // rows of map_kv
+  const int *table, *cu, *kv_len;
   bf16* out;
   float* lse;
+  float *part_o, *part_lse;                // [n_splits][M * H][hd] and [n_splits][M * H] (log2)
   unsigned* err;
 };
 
-// One warp per (row, head): 32 positions at a time, one per lane for the scores, then the lanes share
-// out the head's dimensions for the weighted sum.
 template <int HD>
-__global__ void __launch_bounds__(128) prompt_attention_kernel(const PromptArgs a) {
-  __shared__ float qs[4][HD];
-  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long item = static_cast<long long>(blockIdx.x) * 4 + w;
-  if (item >= static_cast<long long>(a.M) * a.H) return;
-  const int row = static_cast<int>(item / a.H), h = static_cast<int>(item % a.H), hk = h / (a.H / a.Hkv);
-  int lo = 0, hi = a.n_seq;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (a.cu[mid + 1] > row) hi = mid; else lo = mid + 1;
+struct Layout {
+  static constexpr int kSlotBytes = kTile * HD * 2;     // a query tile, or a K or V tile
+  static constexpr int kHalf = kTile * 128;             // its 64-column half
+  static constexpr int kStages = HD == 128 ? 5 : 8;
+  static constexpr int kBytes = (2 + kStages) * kSlotBytes;
+  static constexpr int kSmem = kBytes + 1024 + 256;     // + alignment + barriers
+};
+
+// This CTA's work.
+struct Work {
+  int seq, row0, pos0, kv;                 // sequence, first packed row and its position, positions that exist
+  int tokens[2];                           // of each slot
+  int end[2];                              // positions the slot sees: [0, end)
+  int jb, je;                              // K/V tiles of this split
+};
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+      : "memory");
+}
+// D += A B with A (bf16 pairs, one row per lane) in TMEM.
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(
+          d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Descriptor of an MN-major tile with the 128-byte swizzle: each k is a row of 64 contiguous MN elements
+// (128 bytes), 8 rows per 1024-byte group (stride byte offset between groups along k), the next 64 MN
+// elements `mn_stride` bytes on (leading byte offset).
+__device__ __forceinline__ uint64_t sw128_mn_desc(uint32_t saddr, uint32_t mn_stride) {
+  return (sw128_desc(saddr) & ~(static_cast<uint64_t>(0x3FFF) << 16)) |
+         (static_cast<uint64_t>((mn_stride & 0x3FFFFu) >> 4) << 16);
+}
+
+#define SD2_R16(v, o) "=r"(v[o]), "=r"(v[o + 1]), "=r"(v[o + 2]), "=r"(v[o + 3]), "=r"(v[o + 4]), "=r"(v[o + 5]), \
+    "=r"(v[o + 6]), "=r"(v[o + 7]), "=r"(v[o + 8]), "=r"(v[o + 9]), "=r"(v[o + 10]), "=r"(v[o + 11]),             \
+    "=r"(v[o + 12]), "=r"(v[o + 13]), "=r"(v[o + 14]), "=r"(v[o + 15])
+#define SD2_W16(v, o) "+r"(v[o]), "+r"(v[o + 1]), "+r"(v[o + 2]), "+r"(v[o + 3]), "+r"(v[o + 4]), "+r"(v[o + 5]), \
+    "+r"(v[o + 6]), "+r"(v[o + 7]), "+r"(v[o + 8]), "+r"(v[o + 9]), "+r"(v[o + 10]), "+r"(v[o + 11]),             \
+    "+r"(v[o + 12]), "+r"(v[o + 13]), "+r"(v[o + 14]), "+r"(v[o + 15])
+
+// 32 columns of this thread's TMEM lane; the values are there after ld_wait / ld_tie on the same array.
+__device__ __forceinline__ void ld32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : SD2_R16(r, 0), SD2_R16(r, 16)
+      : "r"(taddr));
+}
+__device__ __forceinline__ void ld_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : SD2_W16(r, 0), SD2_W16(r, 16)::"memory");
+}
+__device__ __forceinline__ void ld_tie(uint32_t (&r)[32]) { asm volatile("" : SD2_W16(r, 0), SD2_W16(r, 16)); }
+__device__ __forceinline__ void st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+
+// Finds the CTA's tile (one warp): tiles are numbered through the sequences, the last of each first (it
+// sees the most positions). False if there is none.
+__device__ bool find_work(const PromptArgs& a, int tile, Work& w) {
+  const int lane = threadIdx.x & 31, per = 2 * a.T;
+  int before = 0;
+  for (int s0 = 0; s0 < a.n_seq; s0 += 32) {
+    const int s = s0 + lane;
+    int lo = 0, hi = 0;
+    if (s < a.n_seq) {
+      lo = min(max(a.cu[s], 0), a.M);
+      hi = min(max(a.cu[s + 1], lo), a.M);
+    }
+    const int n = (hi - lo + per - 1) / per;
+    int sum = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += t;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, before + sum > tile);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      const int n_s = __shfl_sync(0xffffffffu, n, src), end_s = __shfl_sync(0xffffffffu, before + sum, src);
+      const int lo_s = __shfl_sync(0xffffffffu, lo, src), hi_s = __shfl_sync(0xffffffffu, hi, src);
+      const int t = n_s - 1 - (tile - (end_s - n_s));
+      const int rows = hi_s - lo_s, len = a.kv_len[s0 + src];
+      w.seq = s0 + src;
+      w.row0 = lo_s + t * per;
+      w.pos0 = len - rows + t * per;
+      w.kv = min(max(len, 0), a.bt_stride * kPage);
+      int end = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        w.tokens[i] = min(max(rows - t * per - i * a.T, 0), a.T);
+        w.end[i] = w.tokens[i] ? min(max(w.pos0 + i * a.T + w.tokens[i], 0), w.kv) : 0;
+        end = max(end, w.end[i]);
+      }
+      const long long nt = (end + kTile - 1) / kTile;
+      w.jb = static_cast<int>(nt * blockIdx.z / a.n_splits);
+      w.je = static_cast<int>(nt * (blockIdx.z + 1) / a.n_splits);
+      return true;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
   }
-  const int s = lo;
-  if (s >= a.n_seq || a.cu[s] > row) return;
-  const int n_keys = min(a.kv_len[s] - (a.cu[s + 1] - row) + 1, a.bt_stride * kPage);
+  return false;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __grid_constant__ PromptArgs a) {
+  using Lay = Layout<HD>;
+  constexpr int S = Lay::kStages, kHalves = HD / 64;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  __shared__ Work sw;
+  __shared__ int flags[4];                 // [0] abort, [1] TMEM base, [2] work found
+  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 6];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t bar0 = smem_u32(bars);
+  const uint32_t full0 = bar0, empty0 = bar0 + 8 * S, q_full = empty0 + 8 * S, s_full = q_full + 8, p_full = s_full + 16,
+                 drain = p_full + 16;
+  const uint32_t q_smem = smem_u32(smem), kv_smem = q_smem + 2 * Lay::kSlotBytes;
+  volatile int* abort_flag = flags;
+  if (warp == 0) {
+    Work w{};
+    const bool found = find_work(a, blockIdx.x, w);
+    if (lane == 0) {
+      sw = w;
+      flags[0] = 0;
+      flags[2] = found;
+    }
+  } else if (threadIdx.x == 32) {
+    for (int i = 0; i < S; ++i) {
+      mbar_init(full0 + 8 * i, 1);
+      mbar_init(empty0 + 8 * i, 1);
+    }
+    mbar_init(q_full, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full + 8 * i, 1);
+      mbar_init(p_full + 8 * i, 4);
+    }
+    mbar_init(drain, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if (!flags[2]) return;                   // fewer tiles than the grid was sized for
+  if (warp == 9) {
+    tmem_alloc(smem_u32(&flags[1]), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = static_cast<uint32_t>(flags[1]);
+  const int hk = blockIdx.y, jb = sw.jb, je = sw.je;
+  // slot s takes K/V tiles [jb, je_s)
+  const int je0 = min(je, (sw.end[0] + kTile - 1) / kTile), je1 = min(je, (sw.end[1] + kTile - 1) / kTile);
+  const int see = max(sw.end[0], sw.end[1]);
+
+  if (warp == 8) {
+    if (jb < je) {
+      if (lane == 0) {
+        const int slots = (je0 > jb) + (je1 > jb);
+        mbar_expect_tx(q_full, static_cast<uint32_t>(slots * kHalves * a.T * a.G * 128));
+        for (int s = 0; s < 2; ++s)
+          if ((s ? je1 : je0) > jb)
+            for (int h = 0; h < kHalves; ++h)
+              tma_load_3d(q_smem + s * Lay::kSlotBytes + h * Lay::kHalf, &a.map_q, h * 64, hk * a.G, sw.row0 + s * a.T, q_full);
+      }
+      const int page = lane / kHalves, half = lane % kHalves;
+      const int* row = a.table + static_cast<size_t>(sw.seq) * a.bt_stride;
+      const int n_pages = (see + kPage - 1) / kPage;
+      auto id_of = [&](int j) {
+        const int i = j * (kTile / kPage) + page;
+        return page < kTile / kPage && i < n_pages ? row[i] : 0;
+      };
+      int id = id_of(jb);
+      uint32_t u = 0, st = 0, ph = 0;
+      bool ok = true;
+      for (int j = jb; j < je && ok; ++j) {
+        const int np = min(kTile / kPage, n_pages - j * (kTile / kPage));
+        const int next = j + 1 < je ? id_of(j + 1) : 0;
+        const bool bad = id < 0 || id >= a.n_blocks;
+        if (bad && page < np && a.err) atomicOr(a.err, static_cast<unsigned>(ERR_RANGE));
+#pragma unroll
+        for (int v = 0; v < 2; ++v, ++u) {
+          if (!wait_bar(empty0 + 8 * st, ph ^ 1, abort_flag, a.err)) { ok = false; break; }
+          if (lane == 0) mbar_expect_tx(full0 + 8 * st, static_cast<uint32_t>(np * kPage * HD * 2));
+          __syncwarp();
+          if (page < np)                   // a page that does not exist lies outside the map: zeros
+            tma_load_2d(kv_smem + st * Lay::kSlotBytes + half * Lay::kHalf + page * (kPage * 128), &a.map_kv, half * 64,
+                        bad ? a.kv_rows : ((id * 2 + v) * a.Hkv + hk) * kPage, full0 + 8 * st);
+          if (++st == S) { st = 0; ph ^= 1u; }
+        }
+        id = next;
+      }
+      if (!ok) {                           // let the copies in flight land before the CTA exits
+        wait_bar_budget(q_full, 0, kDrainCycles);
+        for (uint32_t i = 0; i < static_cast<uint32_t>(S); ++i)
+          if (i < u) wait_bar_budget(full0 + 8 * i, ((u - 1 - i) / S) & 1, kDrainCycles);
+      }
+    }
+  } else if (warp == 9) {
+    if (jb < je) {
+      const uint32_t idesc_s = idesc_bf16(kTile, 0), idesc_o = idesc_bf16(kTile, HD) | (1u << 16);   // B of P V is MN-major
+      const uint64_t q_desc = sw128_desc(q_smem);
+      bool ok = wait_bar(q_full, 0, abort_flag, a.err);
+      uint32_t st = 0, ph = 0;             // ring position of the next tile to consume
+      auto advance = [&]() { if (++st == S) { st = 0; ph ^= 1u; } };
+      auto scores = [&](int s, int j, uint32_t k_st) {       // S_s = Q_s K_j^T over the pages that the slot sees
+        const int n = min(kTile, (((s ? sw.end[1] : sw.end[0]) - j * kTile) + kPage - 1) / kPage * kPage);
+        const uint32_t id = idesc_s | (static_cast<uint32_t>(n >> 3) << 17);
+        const uint64_t ad = q_desc + ((s * Lay::kSlotBytes) >> 4), bd = sw128_desc(kv_smem + k_st * Lay::kSlotBytes);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+          const uint64_t off = (kk / 4) * (Lay::kHalf >> 4) + (kk % 4) * 2;
+          mma_bf16(tmem + s * kTile, ad + off, bd + off, id, kk > 0);
+        }
+      };
+      if (ok) ok = wait_bar(full0, 0, abort_flag, a.err);
+      if (ok) {
+        tc_fence_after();
+        if (lane == 0) {
+          for (int s = 0; s < 2; ++s)
+            if ((s ? je1 : je0) > jb) {
+              scores(s, jb, 0);
+              mma_commit(s_full + 8 * s);
+            }
+          mma_commit(empty0);
+        }
+        __syncwarp();
+        advance();
+      }
+      for (int j = jb; j < je && ok; ++j) {
+        const uint32_t v_st = st;
+        if (!wait_bar(full0 + 8 * st, ph, abort_flag, a.err)) { ok = false; break; }
+        advance();
+        const uint32_t v_smem = kv_smem + v_st * Lay::kSlotBytes;
+        const int left = see - j * kTile;   // positions of this tile that any row sees
+        if (left < kTile && left % kPage) {
+          // the last page's rows beyond them hold anything (zero probabilities would not mask a NaN)
+          const int r0 = left, r1 = (left + kPage - 1) / kPage * kPage;
+          for (int i = lane; i < (r1 - r0) * 8 * kHalves; i += 32) {
+            const int h = i / ((r1 - r0) * 8), x = i % ((r1 - r0) * 8);
+            *reinterpret_cast<uint4*>(smem + (v_smem - q_smem) + h * Lay::kHalf + r0 * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
+        tc_fence_after();
+        bool have_k = false;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int je_s = s ? je1 : je0;
+          if (j >= je_s || !ok) continue;
+          if (!wait_bar(p_full + 8 * s, (j - jb) & 1, abort_flag, a.err)) { ok = false; continue; }
+          tc_fence_after();
+          if (lane == 0) {
+            const int steps = min(kTile / kPage, ((s ? sw.end[1] : sw.end[0]) - j * kTile + kPage - 1) / kPage);
+            const uint64_t bd = sw128_mn_desc(v_smem, Lay::kHalf);
+            for (int kk = 0; kk < steps; ++kk)
+              mma_bf16_ts(tmem + 2 * kTile + s * HD, tmem + s * kTile + kk * 8, bd + kk * (2048 >> 4), idesc_o,
+                          j > jb || kk > 0);
+          }
+          __syncwarp();
+          if (j + 1 < je_s) {
+            if (!have_k) {
+              if (!wait_bar(full0 + 8 * st, ph, abort_flag, a.err)) { ok = false; continue; }
+              have_k = true;
+              tc_fence_after();
+            }
+            if (lane == 0) scores(s, j + 1, st);
+          }
+          if (lane == 0) mma_commit(s_full + 8 * s);   // S(j + 1) is there, O has tile j
+          __syncwarp();
+        }
+        if (!ok) break;
+        if (lane == 0) {
+          mma_commit(empty0 + 8 * v_st);
+          if (have_k) mma_commit(empty0 + 8 * st);
+        }
+        __syncwarp();
+        if (have_k) advance();
+      }
+      if (lane == 0) mma_commit(drain);    // all products issued by this thread have completed
+      wait_bar_budget(drain, 0, kDrainCycles);
+    }
+  } else {
+    const int s = warp >> 2, r = (warp & 3) * 32 + lane;
+    const int t = r / a.G, g = r - t * a.G;
+    const bool valid = t < (s ? sw.tokens[1] : sw.tokens[0]);
+    const int je_s = s ? je1 : je0;
+    const int see_r = valid ? min(sw.pos0 + s * a.T + t + 1, sw.kv) : 0;   // this row sees positions [0, see_r)
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + lanes + s * kTile, to = tmem + lanes + 2 * kTile + s * HD;
+    const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD));   // scores in log2
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int j = jb; j < je_s; ++j) {
+      if (!wait_bar(s_full + 8 * s, (j - jb) & 1, abort_flag, a.err)) { ok = false; break; }
+      __syncwarp();
+      tc_fence_after();
+      uint32_t x[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) ld32(ts + c * 32, x[c]);
+      ld_wait(x[0]);
+#pragma unroll
+      for (int c = 1; c < 4; ++c) ld_tie(x[c]);
+      const int vis = see_r - j * kTile;   // columns below vis are visible
+      if (vis < kTile) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (c * 32 + i >= vis) x[c][i] = 0xFF800000u;   // -inf
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(x[c][i]));
+      mx *= scale;
+      float f = 1.f;
+      if (mx > m + kGrowth || (m == -INFINITY && mx > m)) {
+        f = ex2(m - mx);
+        m = mx;
+        l *= f;
+      }
+      __syncwarp();
+      if (j > jb && __any_sync(0xffffffffu, f != 1.f)) {
+#pragma unroll
+        for (int c = 0; c < HD / 32; ++c) {
+          uint32_t o[32];
+          ld32(to + c * 32, o);
+          ld_wait(o);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+          st32(to + c * 32, o);
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t p[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float e0 = ex2(__uint_as_float(x[c][2 * i]) * scale - base);
+          const float e1 = ex2(__uint_as_float(x[c][2 * i + 1]) * scale - base);
+          sum[0] += e0;
+          sum[1] += e1;
+          p[i] = pack_bf16(e0, e1);
+        }
+        st16(ts + c * 16, p);
+      }
+      l += sum[0] + sum[1];
+      st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full + 8 * s);
+    }
+    if (je_s > jb && ok) ok = wait_bar(s_full + 8 * s, (je_s - jb) & 1, abort_flag, a.err);
+    __syncwarp();
+    tc_fence_after();
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const size_t item = (static_cast<size_t>(sw.row0) + s * a.T + t) * a.H + hk * a.G + g;
+    const size_t split = static_cast<size_t>(blockIdx.z) * a.M * a.H;
+#pragma unroll
+    for (int c = 0; c < HD / 32; ++c) {
+      uint32_t o[32];
+      ld32(to + c * 32, o);
+      ld_wait(o);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) o[i] = l > 0.f ? __float_as_uint(__uint_as_float(o[i]) * inv) : 0u;
+      if (valid && ok) {
+        if (a.n_splits > 1) {
+          float* dst = a.part_o + (split + item) * HD + c * 32;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(dst + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+        } else {
+          bf16* dst = a.out + item * HD + c * 32;
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              w[e] = pack_bf16(__uint_as_float(o[i + 2 * e]), __uint_as_float(o[i + 2 * e + 1]));
+            *reinterpret_cast<uint4*>(dst + i) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+    }
+    if (valid && ok) {
+      const float l2 = l > 0.f ? m + log2f(l) : -INFINITY;
+      if (a.n_splits > 1) a.part_lse[split + item] = l2;
+      else if (a.lse) a.lse[item] = l2 * 0.6931471805599453f;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+// Joins the splits of each (row, head): o = sum_z w_z o_z / sum_z w_z, w_z = 2^{lse_z - max}. A warp each.
+template <int HD>
+__global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant__ PromptArgs a) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const size_t item = static_cast<size_t>(blockIdx.x) * 4 + (threadIdx.x >> 5), n = static_cast<size_t>(a.M) * a.H;
+  if (item >= n || static_cast<int>(item / a.H) >= a.cu[a.n_seq]) return;
+  float mx = -INFINITY;
+  for (int z = lane; z < a.n_splits; z += 32) mx = fmaxf(mx, a.part_lse[z * n + item]);
+  mx = warp_max(mx);
+  const float base = mx == -INFINITY ? 0.f : mx;
   constexpr int kPer = HD / 32;
-  for (int i = lane; i < HD; i += 32) qs[w][i] = bf2f(a.q[row * a.ldq + h * HD + i]) * (1.f / sqrtf(static_cast<float>(HD)));
-  __syncwarp();
-  float m = -INFINITY, l = 0.f, acc[kPer] = {};
-  for (int j0 = 0; j0 < n_keys; j0 += 32) {
-    const int j = j0 + lane;
-    float z = -INFINITY;
-    int page = 0;
-    if (j < n_keys) {
-      page = a.table[static_cast<size_t>(s) * a.bt_stride + j / kPage];
-      if (page < 0 || page >= a.n_blocks) {
-        if (a.err) atomicOr(a.err, static_cast<unsigned>(ERR_RANGE));
-        page = 0;
-      }
-      const bf16* k = a.pool + ((static_cast<size_t>(page) * 2 * a.Hkv + hk) * kPage + j % kPage) * HD;
-      z = 0.f;
-#pragma unroll 4
-      for (int i = 0; i < HD; i += 8) {
-        const uint4 v = *reinterpret_cast<const uint4*>(k + i);
-        z += bf_lo(v.x) * qs[w][i] + bf_hi(v.x) * qs[w][i + 1] + bf_lo(v.y) * qs[w][i + 2] + bf_hi(v.y) * qs[w][i + 3] +
-             bf_lo(v.z) * qs[w][i + 4] + bf_hi(v.z) * qs[w][i + 5] + bf_lo(v.w) * qs[w][i + 6] + bf_hi(v.w) * qs[w][i + 7];
-      }
-    }
-    const float mn = fmaxf(m, warp_max(z));
-    const float base = mn == -INFINITY ? 0.f : mn;
-    const float p = expf(z - base), f = expf(m - base);
-    m = mn;
-    l = l * f + warp_sum(p);
+  float acc[kPer] = {}, total = 0.f;
+  for (int z = 0; z < a.n_splits; ++z) {
+    const float w = ex2(a.part_lse[z * n + item] - base);
+    total += w;
+    const float* o = a.part_o + (z * n + item) * HD + lane * kPer;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] *= f;
-    for (int t = 0; t < min(32, n_keys - j0); ++t) {
-      const float pt = __shfl_sync(0xffffffffu, p, t);
-      const int pg = __shfl_sync(0xffffffffu, page, t);
-      const bf16* v = a.pool + ((static_cast<size_t>(pg) * 2 * a.Hkv + a.Hkv + hk) * kPage + (j0 + t) % kPage) * HD;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) acc[i] += pt * bf2f(v[i * 32 + lane]);
-    }
+    for (int i = 0; i < kPer; ++i) acc[i] += w * o[i];
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = total > 0.f ? 1.f / total : 0.f;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) a.out[item * HD + i * 32 + lane] = __float2bfloat16_rn(acc[i] * inv);
-  if (a.lse && lane == 0) a.lse[item] = l > 0.f ? m + logf(l) : -INFINITY;
+  for (int i = 0; i < kPer; i += 2)
+    *reinterpret_cast<uint32_t*>(a.out + item * HD + lane * kPer + i) = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
+  if (a.lse && lane == 0) a.lse[item] = total > 0.f ? (mx + log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
 sd2_status fail(sd2_status s, const std::string& m) {
@@ -94,6 +516,33 @@ sd2_status fail(sd2_status s, const std::string& m) {
   return s;
 }
 bool unaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
+
+// The grid: query tiles (an upper bound: the sequences' lengths are on the device), and splits of the
+// positions where tiles x KV heads leave SMs idle; a split keeps at least two K/V tiles.
+struct Shape {
+  int G, T, tiles, splits;
+};
+Shape shape_of(int M, int n_seq, int H, int Hkv, int max_kv) {
+  Shape s;
+  s.G = H / Hkv;
+  s.T = kTile / s.G;
+  s.tiles = static_cast<int>(std::min<long long>(M, M / (2 * s.T) + static_cast<long long>(n_seq)));
+  const long long ctas = static_cast<long long>(s.tiles) * Hkv;
+  const long long most = (max_kv + 2 * kTile - 1) / (2 * kTile);
+  s.splits = static_cast<int>(std::max(1ll, std::min({most, sm_count_cached() / ctas, 128ll})));
+  return s;
+}
+
+template <int HD>
+cudaError_t launch(const PromptArgs& a, int tiles, cudaStream_t st) {
+  constexpr int smem = Layout<HD>::kSmem;
+  cudaError_t e = cudaFuncSetAttribute(prompt_attention_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  prompt_attention_kernel<HD><<<dim3(tiles, a.Hkv, a.n_splits), kThreads, smem, st>>>(a);
+  if ((e = cudaGetLastError()) != cudaSuccess || a.n_splits == 1) return e;
+  const unsigned grid = static_cast<unsigned>((static_cast<long long>(a.M) * a.H + 3) / 4);
+  return launch_pdl(prompt_join_kernel<HD>, dim3(grid), dim3(128), 0, st, a);
+}
 
 }  // namespace
 }  // namespace sd2
@@ -104,7 +553,9 @@ using namespace sd2;
 
 size_t sd2_attention_prompt_workspace_bytes(int32_t M, int32_t n_seq, int32_t H, int32_t Hkv, int32_t hd, int32_t max_kv) {
   if (M < 1 || n_seq < 1 || Hkv < 1 || H < Hkv || H % Hkv || (hd != 64 && hd != 128) || max_kv < 1) return 0;
-  return 256;
+  const Shape s = shape_of(M, n_seq, H, Hkv, max_kv);
+  const size_t parts = s.splits > 1 ? static_cast<size_t>(s.splits) * M * H * (hd + 1) * 4 : 0;
+  return 256 + (parts + 255) / 256 * 256;
 }
 
 sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t H, int32_t Hkv, int32_t hd,
@@ -118,7 +569,7 @@ sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t
     return fail(SD2_EINVAL, "bad attention shape (hd 64 or 128, H a multiple of Hkv, at most 128 heads per KV head)");
   if (n_blocks < 1 || bt_stride < 1 || bt_stride > (1 << 26) || layer < 0 || n_seq < 1 || max_kv < 1)
     return fail(SD2_EINVAL, "need n_blocks, bt_stride, n_seq, max_kv >= 1, bt_stride <= 2^26 and layer >= 0");
-  if (static_cast<int64_t>(n_blocks) * 2 * Hkv * kPage > INT32_MAX)
+  if (Hkv > 65535 || static_cast<int64_t>(n_blocks) * 2 * Hkv * kPage > INT32_MAX)
     return fail(SD2_EINVAL, "a layer's K/V rows must be countable in 31 bits");
   if (ldq < static_cast<int64_t>(H) * hd || ldq % 8 || unaligned(d_q, 16) || unaligned(d_pool, 16) || unaligned(d_out, 16))
     return fail(SD2_EINVAL, "q rows, pool and out must be 16-byte aligned, ldq >= H * hd");
@@ -126,16 +577,21 @@ sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t
     return fail(SD2_EINVAL, "workspace too small");
   if (unaligned(d_workspace, 256)) return fail(SD2_EINVAL, "workspace not 256-byte aligned");
   if (M == 0) return SD2_OK;
+  const Shape s = shape_of(M, n_seq, H, Hkv, max_kv);
   PromptArgs a{};
-  a.q = static_cast<const bf16*>(d_q); a.ldq = ldq; a.M = M; a.H = H; a.Hkv = Hkv;
-  a.pool = static_cast<const bf16*>(d_pool) + static_cast<size_t>(layer) * n_blocks * 2 * Hkv * kPage * hd;
-  a.n_blocks = n_blocks; a.table = d_table; a.bt_stride = bt_stride; a.cu = d_cu_rows; a.kv_len = d_kv_len;
-  a.n_seq = n_seq; a.out = static_cast<bf16*>(d_out); a.lse = d_lse; a.err = d_err;
+  a.M = M; a.H = H; a.Hkv = Hkv; a.G = s.G; a.T = s.T; a.n_blocks = n_blocks; a.bt_stride = bt_stride;
+  a.n_seq = n_seq; a.n_splits = s.splits; a.kv_rows = n_blocks * 2 * Hkv * kPage;
+  a.table = d_table; a.cu = d_cu_rows; a.kv_len = d_kv_len; a.out = static_cast<bf16*>(d_out); a.lse = d_lse;
+  // the workspace: a stand-in for the error word, then the splits' partial results
+  a.err = d_err ? d_err : static_cast<unsigned*>(d_workspace);
+  a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(d_workspace) + 256);
+  a.part_lse = a.part_o + static_cast<size_t>(s.splits) * M * H * hd;
+  const bf16* pool = static_cast<const bf16*>(d_pool) + static_cast<size_t>(layer) * n_blocks * 2 * Hkv * kPage * hd;
+  if (!encode_weight_map(&a.map_kv, pool, a.kv_rows, hd, kPage) ||
+      !encode_rows_map(&a.map_q, d_q, hd, H, M, ldq, s.G, s.T))
+    return fail(SD2_ECUDA, "prompt attention: tensor map");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const unsigned grid = static_cast<unsigned>((static_cast<long long>(M) * H + 3) / 4);
-  if (hd == 64) prompt_attention_kernel<64><<<grid, 128, 0, st>>>(a);
-  else prompt_attention_kernel<128><<<grid, 128, 0, st>>>(a);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = hd == 64 ? launch<64>(a, s.tiles, st) : launch<128>(a, s.tiles, st);
   return e == cudaSuccess ? SD2_OK : fail(SD2_ECUDA, std::string("prompt attention launch: ") + cudaGetErrorString(e));
 }
 
