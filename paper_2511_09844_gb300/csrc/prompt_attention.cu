@@ -37,7 +37,8 @@ using namespace tc;
 
 constexpr int kPage = 16;
 constexpr int kTile = 128;                 // positions per K/V tile, query vectors per slot
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;             // three warpgroups: 168 registers each at launch, then 216 / 216 / 72
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;    // 2 x 128 x 216 + 128 x 72 = 384 x 168
 constexpr int kMaxStages = 8;
 constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum that makes O be rescaled
 
@@ -136,9 +137,37 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Two fp32 operations per instruction: a * b + c and a + b on packed pairs.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+  return v;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+  return v;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&t);
+}
+
+// True in one thread of the (converged) warp: the compiler then knows that the code under it runs in a single
+// thread and keeps the MMA operands in uniform registers (under a lane == 0 test each MMA took 125 cycles to
+// issue, more than it runs).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p != 0;
 }
 
 // Finds the CTA's tile (one warp): tiles are numbered through the sequences, the last of each first (it
@@ -196,11 +225,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   __shared__ Work sw;
   __shared__ int flags[4];                 // [0] abort, [1] TMEM base, [2] work found
-  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 6];
+  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t bar0 = smem_u32(bars);
   const uint32_t full0 = bar0, empty0 = bar0 + 8 * S, q_full = empty0 + 8 * S, s_full = q_full + 8, p_full = s_full + 16,
-                 drain = p_full + 16;
+                 drain = p_full + 32;
   const uint32_t q_smem = smem_u32(smem), kv_smem = q_smem + 2 * Lay::kSlotBytes;
   volatile int* abort_flag = flags;
   if (warp == 0) {
@@ -219,7 +248,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
     mbar_init(q_full, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + 8 * i, 1);
-      mbar_init(p_full + 8 * i, 4);
+      mbar_init(p_full + 16 * i, 4);
+      mbar_init(p_full + 16 * i + 8, 4);
     }
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -239,8 +269,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
   const int je0 = min(je, (sw.end[0] + kTile - 1) / kTile), je1 = min(je, (sw.end[1] + kTile - 1) / kTile);
   const int see = max(sw.end[0], sw.end[1]);
 
-  if (warp == 8) {
-    if (jb < je) {
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == 8 && jb < je) {
       if (lane == 0) {
         const int slots = (je0 > jb) + (je1 > jb);
         mbar_expect_tx(q_full, static_cast<uint32_t>(slots * kHalves * a.T * a.G * 128));
@@ -281,9 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         for (uint32_t i = 0; i < static_cast<uint32_t>(S); ++i)
           if (i < u) wait_bar_budget(full0 + 8 * i, ((u - 1 - i) / S) & 1, kDrainCycles);
       }
-    }
-  } else if (warp == 9) {
-    if (jb < je) {
+    } else if (warp == 9 && jb < je && elect_one()) {
       const uint32_t idesc_s = idesc_bf16(kTile, 0), idesc_o = idesc_bf16(kTile, HD) | (1u << 16);   // B of P V is MN-major
       const uint64_t q_desc = sw128_desc(q_smem);
       bool ok = wait_bar(q_full, 0, abort_flag, a.err);
@@ -302,15 +331,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       if (ok) ok = wait_bar(full0, 0, abort_flag, a.err);
       if (ok) {
         tc_fence_after();
-        if (lane == 0) {
-          for (int s = 0; s < 2; ++s)
-            if ((s ? je1 : je0) > jb) {
-              scores(s, jb, 0);
-              mma_commit(s_full + 8 * s);
-            }
-          mma_commit(empty0);
-        }
-        __syncwarp();
+        for (int s = 0; s < 2; ++s)
+          if ((s ? je1 : je0) > jb) {
+            scores(s, jb, 0);
+            mma_commit(s_full + 8 * s);
+          }
+        mma_commit(empty0);
         advance();
       }
       for (int j = jb; j < je && ok; ++j) {
@@ -322,12 +348,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         if (left < kTile && left % kPage) {
           // the last page's rows beyond them hold anything (zero probabilities would not mask a NaN)
           const int r0 = left, r1 = (left + kPage - 1) / kPage * kPage;
-          for (int i = lane; i < (r1 - r0) * 8 * kHalves; i += 32) {
+          for (int i = 0; i < (r1 - r0) * 8 * kHalves; ++i) {
             const int h = i / ((r1 - r0) * 8), x = i % ((r1 - r0) * 8);
             *reinterpret_cast<uint4*>(smem + (v_smem - q_smem) + h * Lay::kHalf + r0 * 128 + x * 16) = make_uint4(0, 0, 0, 0);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
         }
         tc_fence_after();
         bool have_k = false;
@@ -335,39 +360,41 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         for (int s = 0; s < 2; ++s) {
           const int je_s = s ? je1 : je0;
           if (j >= je_s || !ok) continue;
-          if (!wait_bar(p_full + 8 * s, (j - jb) & 1, abort_flag, a.err)) { ok = false; continue; }
-          tc_fence_after();
-          if (lane == 0) {
-            const int steps = min(kTile / kPage, ((s ? sw.end[1] : sw.end[0]) - j * kTile + kPage - 1) / kPage);
-            const uint64_t bd = sw128_mn_desc(v_smem, Lay::kHalf);
-            for (int kk = 0; kk < steps; ++kk)
-              mma_bf16_ts(tmem + 2 * kTile + s * HD, tmem + s * kTile + kk * 8, bd + kk * (2048 >> 4), idesc_o,
-                          j > jb || kk > 0);
+          const int steps = min(kTile / kPage, ((s ? sw.end[1] : sw.end[0]) - j * kTile + kPage - 1) / kPage);
+          const uint64_t bd = sw128_mn_desc(v_smem, Lay::kHalf);
+#pragma unroll
+          for (int part = 0; part < 2; ++part) {             // the halves of P as they come
+            if (!ok || !wait_bar(p_full + 16 * s + 8 * part, (j - jb) & 1, abort_flag, a.err)) { ok = false; continue; }
+            tc_fence_after();
+#pragma unroll
+            for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
+              if (kk < steps)
+                mma_bf16_ts(tmem + 2 * kTile + s * HD, tmem + s * kTile + kk * 8, bd + kk * (2048 >> 4), idesc_o,
+                            j > jb || kk > 0);
           }
-          __syncwarp();
+          if (!ok) continue;
           if (j + 1 < je_s) {
             if (!have_k) {
               if (!wait_bar(full0 + 8 * st, ph, abort_flag, a.err)) { ok = false; continue; }
               have_k = true;
               tc_fence_after();
             }
-            if (lane == 0) scores(s, j + 1, st);
+            scores(s, j + 1, st);
           }
-          if (lane == 0) mma_commit(s_full + 8 * s);   // S(j + 1) is there, O has tile j
-          __syncwarp();
+          mma_commit(s_full + 8 * s);      // S(j + 1) is there, O has tile j
         }
         if (!ok) break;
-        if (lane == 0) {
-          mma_commit(empty0 + 8 * v_st);
-          if (have_k) mma_commit(empty0 + 8 * st);
+        mma_commit(empty0 + 8 * v_st);
+        if (have_k) {
+          mma_commit(empty0 + 8 * st);
+          advance();
         }
-        __syncwarp();
-        if (have_k) advance();
       }
-      if (lane == 0) mma_commit(drain);    // all products issued by this thread have completed
+      mma_commit(drain);                   // all products issued by this thread have completed
       wait_bar_budget(drain, 0, kDrainCycles);
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int s = warp >> 2, r = (warp & 3) * 32 + lane;
     const int t = r / a.G, g = r - t * a.G;
     const bool valid = t < (s ? sw.tokens[1] : sw.tokens[0]);
@@ -396,11 +423,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           for (int i = 0; i < 32; ++i)
             if (c * 32 + i >= vis) x[c][i] = 0xFF800000u;   // -inf
       }
-      float mx = -INFINITY;
+      float top[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int c = 0; c < 4; ++c) {
+        top[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
 #pragma unroll
-        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(x[c][i]));
+        for (int i = 2; i < 32; i += 2) top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])));
+      }
+      float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
       mx *= scale;
       float f = 1.f;
       if (mx > m + kGrowth || (m == -INFINITY && mx > m)) {
@@ -421,25 +451,31 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         }
       }
       const float base = m == -INFINITY ? 0.f : m;
-      float sum[2] = {0.f, 0.f};
+      const uint64_t scale2 = pair(scale, scale), base2 = pair(-base, -base);
+      uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         uint32_t p[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float e0 = ex2(__uint_as_float(x[c][2 * i]) * scale - base);
-          const float e1 = ex2(__uint_as_float(x[c][2 * i + 1]) * scale - base);
-          sum[0] += e0;
-          sum[1] += e1;
+          float e0, e1;
+          unpair(fma2(pair(__uint_as_float(x[c][2 * i]), __uint_as_float(x[c][2 * i + 1])), scale2, base2), e0, e1);
+          e0 = ex2(e0);
+          e1 = ex2(e1);
+          sum[i & 1] = add2(sum[i & 1], pair(e0, e1));
           p[i] = pack_bf16(e0, e1);
         }
         st16(ts + c * 16, p);
+        if (c & 1) {                       // half of the tile's probabilities are there
+          st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * (c >> 1));
+        }
       }
-      l += sum[0] + sum[1];
-      st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(p_full + 8 * s);
+      float s0, s1;
+      unpair(add2(sum[0], sum[1]), s0, s1);
+      l += s0 + s1;
     }
     if (je_s > jb && ok) ok = wait_bar(s_full + 8 * s, (je_s - jb) & 1, abort_flag, a.err);
     __syncwarp();
