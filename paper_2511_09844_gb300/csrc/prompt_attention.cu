@@ -50,7 +50,7 @@ struct PromptArgs {
   const int *table, *cu, *kv_len;
   bf16* out;
   float* lse;
-  float *part_o, *part_lse;                // [n_splits][M * H][hd] and [n_splits][M * H] (log2)
+  float *part_o, *part_lse;                // [2 n_splits][M * H][hd] and [2 n_splits][M * H] (log2)
   unsigned* err;
 };
 
@@ -63,9 +63,11 @@ struct Layout {
   static constexpr int kSmem = kBytes + 1024 + 256;     // + alignment + barriers
 };
 
-// This CTA's work.
+// One piece of work: two query tiles (slots) of a sequence and KV head against some of its K/V tiles.
 struct Work {
-  int seq, row0, pos0, kv;                 // sequence, first packed row and its position, positions that exist
+  int seq, hk, split;                      // seq < 0: no more work
+  int row0, pos0, kv;                      // first packed row and its position, positions that exist
+  int solo;                                // both slots hold slot 0's tokens and take K/V tiles in turn
   int tokens[2];                           // of each slot
   int end[2];                              // positions the slot sees: [0, end)
   int jb, je;                              // K/V tiles of this split
@@ -170,52 +172,84 @@ __device__ __forceinline__ bool elect_one() {
   return p != 0;
 }
 
-// Finds the CTA's tile (one warp): tiles are numbered through the sequences, the last of each first (it
-// sees the most positions). False if there is none.
-__device__ bool find_work(const PromptArgs& a, int tile, Work& w) {
-  const int lane = threadIdx.x & 31, per = 2 * a.T;
-  int before = 0;
-  for (int s0 = 0; s0 < a.n_seq; s0 += 32) {
-    const int s = s0 + lane;
-    int lo = 0, hi = 0;
+// Finds tile `tile` of the grid (one warp): tiles are numbered through the sequences, the last of each first
+// (it sees the most positions). The first 32 sequences stay in the lanes' registers.
+struct Finder {
+  int lo, hi, len, n, sum;                 // this lane's sequence: packed rows, cached length, tiles; inclusive sum of n
+  __device__ __forceinline__ void load(const PromptArgs& a, int s) {
+    lo = hi = len = 0;
     if (s < a.n_seq) {
       lo = min(max(a.cu[s], 0), a.M);
       hi = min(max(a.cu[s + 1], lo), a.M);
+      len = a.kv_len[s];
     }
-    const int n = (hi - lo + per - 1) / per;
-    int sum = n;
+    n = (hi - lo + 2 * a.T - 1) / (2 * a.T);
+    sum = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int t = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += t;
+      if ((threadIdx.x & 31) >= o) sum += t;
     }
-    const unsigned hit = __ballot_sync(0xffffffffu, before + sum > tile);
+  }
+};
+__device__ bool find_work(const PromptArgs& a, const Finder& first, int tile, int hk, int split, Work& w) {
+  const int lane = threadIdx.x & 31, per = 2 * a.T;
+  Finder f = first;
+  int before = 0;
+  for (int s0 = 0; s0 < a.n_seq; s0 += 32) {
+    if (s0) f.load(a, s0 + lane);
+    const unsigned hit = __ballot_sync(0xffffffffu, before + f.sum > tile);
     if (hit) {
       const int src = __ffs(hit) - 1;
-      const int n_s = __shfl_sync(0xffffffffu, n, src), end_s = __shfl_sync(0xffffffffu, before + sum, src);
-      const int lo_s = __shfl_sync(0xffffffffu, lo, src), hi_s = __shfl_sync(0xffffffffu, hi, src);
-      const int t = n_s - 1 - (tile - (end_s - n_s));
-      const int rows = hi_s - lo_s, len = a.kv_len[s0 + src];
+      const int n_s = __shfl_sync(0xffffffffu, f.n, src), end_s = before + __shfl_sync(0xffffffffu, f.sum, src);
+      const int lo_s = __shfl_sync(0xffffffffu, f.lo, src), hi_s = __shfl_sync(0xffffffffu, f.hi, src);
+      const int len = __shfl_sync(0xffffffffu, f.len, src);
+      const int t = n_s - 1 - (tile - (end_s - n_s)), rows = hi_s - lo_s;
       w.seq = s0 + src;
+      w.hk = hk;
+      w.split = split;
       w.row0 = lo_s + t * per;
       w.pos0 = len - rows + t * per;
       w.kv = min(max(len, 0), a.bt_stride * kPage);
-      int end = 0;
+      w.solo = a.n_splits > 1 && rows - t * per <= a.T;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        w.tokens[i] = min(max(rows - t * per - i * a.T, 0), a.T);
-        w.end[i] = w.tokens[i] ? min(max(w.pos0 + i * a.T + w.tokens[i], 0), w.kv) : 0;
-        end = max(end, w.end[i]);
+        const int from = w.solo ? 0 : i * a.T;
+        w.tokens[i] = min(max(rows - t * per - from, 0), a.T);
+        w.end[i] = w.tokens[i] ? min(max(w.pos0 + from + w.tokens[i], 0), w.kv) : 0;
       }
-      const long long nt = (end + kTile - 1) / kTile;
-      w.jb = static_cast<int>(nt * blockIdx.z / a.n_splits);
-      w.je = static_cast<int>(nt * (blockIdx.z + 1) / a.n_splits);
+      const long long nt = (max(w.end[0], w.end[1]) + kTile - 1) / kTile;
+      w.jb = static_cast<int>(nt * split / a.n_splits);
+      w.je = static_cast<int>(nt * (split + 1) / a.n_splits);
       return true;
     }
-    before += __shfl_sync(0xffffffffu, sum, 31);
+    before += __shfl_sync(0xffffffffu, f.sum, 31);
   }
   return false;
 }
+
+// Cluster launch control: asks for a block of this grid that has not started yet; the answer (16 bytes)
+// comes with the barrier's transaction.
+__device__ __forceinline__ void request_block(uint32_t answer, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer),
+               "r"(bar)
+               : "memory");
+}
+// Whether a block was given, and its index.
+__device__ __forceinline__ bool read_block(uint32_t answer, int& x, int& y, int& z) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b128 h;\n ld.shared.b128 h, [%4];\n"
+      " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n selp.u32 %0, 1, 0, p;\n"
+      " mov.u32 %1, 0;\n mov.u32 %2, 0;\n mov.u32 %3, 0;\n"
+      " @p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, %2, %3, _}, h;\n}"
+      : "=r"(ok), "=r"(x), "=r"(y), "=r"(z)
+      : "r"(answer)
+      : "memory");
+  return ok != 0;
+}
+
+constexpr int kConsumers = 10;             // of a piece of work: the loader, the MMA thread, 8 softmax warps
 
 template <int HD>
 __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __grid_constant__ PromptArgs a) {
@@ -223,295 +257,413 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
   constexpr int S = Lay::kStages, kHalves = HD / 64;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  __shared__ Work sw;
-  __shared__ int flags[4];                 // [0] abort, [1] TMEM base, [2] work found
-  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 8];
+  __shared__ Work works[2];
+  __shared__ __align__(16) uint4 answer;
+  __shared__ int flags[2];                 // [0] abort, [1] TMEM base
+  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t bar0 = smem_u32(bars);
-  const uint32_t full0 = bar0, empty0 = bar0 + 8 * S, q_full = empty0 + 8 * S, s_full = q_full + 8, p_full = s_full + 16,
-                 drain = p_full + 32;
+  const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * S, q_full = empty0 + 8 * S, q_empty = q_full + 8,
+                 s_full = q_empty + 8, o_full = s_full + 16, p_full = o_full + 16, drain = p_full + 32,
+                 w_full = drain + 8, w_empty = w_full + 16, w_taken = w_empty + 16, given = w_taken + 8;
   const uint32_t q_smem = smem_u32(smem), kv_smem = q_smem + 2 * Lay::kSlotBytes;
   volatile int* abort_flag = flags;
-  if (warp == 0) {
-    Work w{};
-    const bool found = find_work(a, blockIdx.x, w);
-    if (lane == 0) {
-      sw = w;
-      flags[0] = 0;
-      flags[2] = found;
-    }
-  } else if (threadIdx.x == 32) {
+  if (a.n_splits > 1) pdl_trigger();       // the join may be set up (it waits for this grid to complete)
+  Work first{};
+  Finder finder{};
+  bool found = false;
+  if (warp == 10) {
+    finder.load(a, lane);
+    found = find_work(a, finder, blockIdx.x, blockIdx.y, blockIdx.z, first);
+  } else if (warp == 9) {
+    tmem_alloc(smem_u32(&flags[1]), 512);
+    tmem_relinquish();
+  } else if (warp == 8) {
+    if (lane < 2)
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &a.map_q : &a.map_kv)) : "memory");
+  } else if (threadIdx.x == 0) {
+    flags[0] = 0;
     for (int i = 0; i < S; ++i) {
       mbar_init(full0 + 8 * i, 1);
       mbar_init(empty0 + 8 * i, 1);
     }
     mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + 8 * i, 1);
+      mbar_init(o_full + 8 * i, 1);
       mbar_init(p_full + 16 * i, 4);
       mbar_init(p_full + 16 * i + 8, 4);
+      mbar_init(w_full + 8 * i, 1);
+      mbar_init(w_empty + 8 * i, kConsumers);
     }
     mbar_init(drain, 1);
+    mbar_init(w_taken, 1);
+    mbar_init(given, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  __syncthreads();
-  if (!flags[2]) return;                   // fewer tiles than the grid was sized for
-  if (warp == 9) {
-    tmem_alloc(smem_u32(&flags[1]), 512);
-    tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = static_cast<uint32_t>(flags[1]);
-  const int hk = blockIdx.y, jb = sw.jb, je = sw.je;
-  // slot s takes K/V tiles [jb, je_s)
-  const int je0 = min(je, (sw.end[0] + kTile - 1) / kTile), je1 = min(je, (sw.end[1] + kTile - 1) / kTile);
-  const int see = max(sw.end[0], sw.end[1]);
+  // the next piece of work, for each consumer; false when there is none (or a wait has given up)
+  auto wait_one = [&](uint32_t bar, uint32_t parity) { return wait_bar(bar, parity, abort_flag, a.err); };
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_one(bar, parity)) != 0; };
+  uint32_t n_work = 0;
+  auto next_work = [&](Work& w, auto wait) {
+    const uint32_t i = n_work & 1;
+    if (!wait(w_full + 8 * i, (n_work >> 1) & 1)) return false;
+    w = works[i];
+    ++n_work;
+    return w.seq >= 0;
+  };
+  auto done_reading = [&]() { mbar_arrive(w_empty + 8 * ((n_work - 1) & 1)); };
+  // K/V tiles slot s takes: from jb (+ 1 for slot 1 of solo work) in steps of 1 (2) below
+  auto last_tile = [](const Work& w, int s) { return min(w.je, (w.end[s] + kTile - 1) / kTile); };
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == 8 && jb < je) {
-      if (lane == 0) {
-        const int slots = (je0 > jb) + (je1 > jb);
-        mbar_expect_tx(q_full, static_cast<uint32_t>(slots * kHalves * a.T * a.G * 128));
-        for (int s = 0; s < 2; ++s)
-          if ((s ? je1 : je0) > jb)
-            for (int h = 0; h < kHalves; ++h)
-              tma_load_3d(q_smem + s * Lay::kSlotBytes + h * Lay::kHalf, &a.map_q, h * 64, hk * a.G, sw.row0 + s * a.T, q_full);
-      }
+    if (warp == 8) {
+      Work w;
       const int page = lane / kHalves, half = lane % kHalves;
-      const int* row = a.table + static_cast<size_t>(sw.seq) * a.bt_stride;
-      const int n_pages = (see + kPage - 1) / kPage;
-      auto id_of = [&](int j) {
-        const int i = j * (kTile / kPage) + page;
-        return page < kTile / kPage && i < n_pages ? row[i] : 0;
-      };
-      int id = id_of(jb);
-      uint32_t u = 0, st = 0, ph = 0;
+      uint32_t u = 0, st = 0, ph = 0, n_q = 0;
       bool ok = true;
-      for (int j = jb; j < je && ok; ++j) {
-        const int np = min(kTile / kPage, n_pages - j * (kTile / kPage));
-        const int next = j + 1 < je ? id_of(j + 1) : 0;
-        const bool bad = id < 0 || id >= a.n_blocks;
-        if (bad && page < np && a.err) atomicOr(a.err, static_cast<unsigned>(ERR_RANGE));
-#pragma unroll
-        for (int v = 0; v < 2; ++v, ++u) {
-          if (!wait_bar(empty0 + 8 * st, ph ^ 1, abort_flag, a.err)) { ok = false; break; }
+      while (ok && next_work(w, wait_warp)) {
+        __syncwarp();
+        if (lane == 0) {
+          done_reading();
+          mbar_arrive(w_taken);
+        }
+        if (w.jb >= w.je) continue;
+        const int* row = a.table + static_cast<size_t>(w.seq) * a.bt_stride;
+        const int see = max(w.end[0], w.end[1]), n_pages = (see + kPage - 1) / kPage, step = 1 + w.solo;
+        auto id_of = [&](int j) {
+          const int i = j * (kTile / kPage) + page;
+          return j < w.je && page < kTile / kPage && i < n_pages ? row[i] : 0;
+        };
+        int id[3];                           // page ids of tiles j, j + 1, j + 2
+        id[0] = id_of(w.jb);
+        id[1] = id_of(w.jb + 1);
+        // Q once the last piece's scores are done
+        if (!(ok = wait_warp(q_empty, (n_q & 1) ^ 1))) break;
+        if (lane == 0) {
+          const int slots = !w.solo && last_tile(w, 0) > w.jb && last_tile(w, 1) > w.jb ? 2 : 1;
+          const int s0 = !w.solo && last_tile(w, 0) <= w.jb ? 1 : 0;
+          mbar_expect_tx(q_full, static_cast<uint32_t>(slots * kHalves * a.T * a.G * 128));
+          for (int s = s0; s < s0 + slots; ++s)
+            for (int h = 0; h < kHalves; ++h)
+              tma_load_3d(q_smem + s * Lay::kSlotBytes + h * Lay::kHalf, &a.map_q, h * 64, w.hk * a.G, w.row0 + s * a.T, q_full);
+        }
+        ++n_q;
+        auto load = [&](int j, int v, int page_id) {
+          const int np = min(kTile / kPage, n_pages - j * (kTile / kPage));
+          const bool bad = page_id < 0 || page_id >= a.n_blocks;
+          if (bad && page < np && a.err) atomicOr(a.err, static_cast<unsigned>(ERR_RANGE));
+          if (!wait_warp(empty0 + 8 * st, ph ^ 1)) return false;
           if (lane == 0) mbar_expect_tx(full0 + 8 * st, static_cast<uint32_t>(np * kPage * HD * 2));
           __syncwarp();
-          if (page < np)                   // a page that does not exist lies outside the map: zeros
+          if (page < np)                     // a page that does not exist lies outside the map: zeros
             tma_load_2d(kv_smem + st * Lay::kSlotBytes + half * Lay::kHalf + page * (kPage * 128), &a.map_kv, half * 64,
-                        bad ? a.kv_rows : ((id * 2 + v) * a.Hkv + hk) * kPage, full0 + 8 * st);
+                        bad ? a.kv_rows : ((page_id * 2 + v) * a.Hkv + w.hk) * kPage, full0 + 8 * st);
           if (++st == S) { st = 0; ph ^= 1u; }
+          ++u;
+          return true;
+        };
+        ok = load(w.jb, 0, id[0]);
+        if (ok && step == 2 && w.jb + 1 < w.je) ok = load(w.jb + 1, 0, id[1]);
+        for (int j = w.jb; j < w.je && ok; ++j) {
+          id[2] = id_of(j + 2);
+          ok = load(j, 1, id[0]);
+          if (ok && j + step < w.je) ok = load(j + step, 0, step == 2 ? id[2] : id[1]);
+          id[0] = id[1];
+          id[1] = id[2];
         }
-        id = next;
       }
-      if (!ok) {                           // let the copies in flight land before the CTA exits
-        wait_bar_budget(q_full, 0, kDrainCycles);
+      if (*abort_flag) {                     // let the copies in flight land before the CTA exits
+        if (n_q) wait_bar_budget(q_full, (n_q - 1) & 1, kDrainCycles);
         for (uint32_t i = 0; i < static_cast<uint32_t>(S); ++i)
           if (i < u) wait_bar_budget(full0 + 8 * i, ((u - 1 - i) / S) & 1, kDrainCycles);
       }
-    } else if (warp == 9 && jb < je && elect_one()) {
-      const uint32_t idesc_s = idesc_bf16(kTile, 0), idesc_o = idesc_bf16(kTile, HD) | (1u << 16);   // B of P V is MN-major
-      const uint64_t q_desc = sw128_desc(q_smem);
-      bool ok = wait_bar(q_full, 0, abort_flag, a.err);
-      uint32_t st = 0, ph = 0;             // ring position of the next tile to consume
-      auto advance = [&]() { if (++st == S) { st = 0; ph ^= 1u; } };
-      auto scores = [&](int s, int j, uint32_t k_st) {       // S_s = Q_s K_j^T over the pages that the slot sees
-        const int n = min(kTile, (((s ? sw.end[1] : sw.end[0]) - j * kTile) + kPage - 1) / kPage * kPage);
-        const uint32_t id = idesc_s | (static_cast<uint32_t>(n >> 3) << 17);
-        const uint64_t ad = q_desc + ((s * Lay::kSlotBytes) >> 4), bd = sw128_desc(kv_smem + k_st * Lay::kSlotBytes);
+    } else if (warp == 9) {
+      if (elect_one()) {
+        const uint32_t idesc_s = idesc_bf16(kTile, 0), idesc_o = idesc_bf16(kTile, HD) | (1u << 16);   // B of P V is MN-major
+        const uint64_t q_desc = sw128_desc(q_smem);
+        Work w;
+        bool ok = true;
+        uint32_t st = 0, ph = 0, n_q = 0, n_p[2] = {0, 0};     // ring position of the next tile, Q tiles, P tiles so far
+        auto advance = [&]() { if (++st == S) { st = 0; ph ^= 1u; } };
+        while (ok && next_work(w, wait_one)) {
+          done_reading();
+          if (w.jb >= w.je) continue;
+          const int step = 1 + w.solo;
+          const int last[2] = {last_tile(w, 0), last_tile(w, 1)};
+          auto active = [&](int s, int j) { return j < last[s] && (!w.solo || ((j - w.jb) & 1) == s); };
+          auto scores = [&](int s, int j, uint32_t k_st) {     // S_s = Q_s K_j^T over the pages that the slot sees
+            const int n = min(kTile, ((s ? w.end[1] : w.end[0]) - j * kTile + kPage - 1) / kPage * kPage);
+            const uint32_t id = idesc_s | (static_cast<uint32_t>(n >> 3) << 17);
+            const uint64_t ad = q_desc + (w.solo ? 0 : (s * Lay::kSlotBytes) >> 4), bd = sw128_desc(kv_smem + k_st * Lay::kSlotBytes);
 #pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk) {
-          const uint64_t off = (kk / 4) * (Lay::kHalf >> 4) + (kk % 4) * 2;
-          mma_bf16(tmem + s * kTile, ad + off, bd + off, id, kk > 0);
-        }
-      };
-      if (ok) ok = wait_bar(full0, 0, abort_flag, a.err);
-      if (ok) {
-        tc_fence_after();
-        for (int s = 0; s < 2; ++s)
-          if ((s ? je1 : je0) > jb) {
-            scores(s, jb, 0);
+            for (int kk = 0; kk < HD / 16; ++kk) {
+              const uint64_t off = (kk / 4) * (Lay::kHalf >> 4) + (kk % 4) * 2;
+              mma_bf16(tmem + s * kTile, ad + off, bd + off, id, kk > 0);
+            }
             mma_commit(s_full + 8 * s);
-          }
-        mma_commit(empty0);
-        advance();
-      }
-      for (int j = jb; j < je && ok; ++j) {
-        const uint32_t v_st = st;
-        if (!wait_bar(full0 + 8 * st, ph, abort_flag, a.err)) { ok = false; break; }
-        advance();
-        const uint32_t v_smem = kv_smem + v_st * Lay::kSlotBytes;
-        const int left = see - j * kTile;   // positions of this tile that any row sees
-        if (left < kTile && left % kPage) {
-          // the last page's rows beyond them hold anything (zero probabilities would not mask a NaN)
-          const int r0 = left, r1 = (left + kPage - 1) / kPage * kPage;
-          for (int i = 0; i < (r1 - r0) * 8 * kHalves; ++i) {
-            const int h = i / ((r1 - r0) * 8), x = i % ((r1 - r0) * 8);
-            *reinterpret_cast<uint4*>(smem + (v_smem - q_smem) + h * Lay::kHalf + r0 * 128 + x * 16) = make_uint4(0, 0, 0, 0);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        }
-        tc_fence_after();
-        bool have_k = false;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const int je_s = s ? je1 : je0;
-          if (j >= je_s || !ok) continue;
-          const int steps = min(kTile / kPage, ((s ? sw.end[1] : sw.end[0]) - j * kTile + kPage - 1) / kPage);
-          const uint64_t bd = sw128_mn_desc(v_smem, Lay::kHalf);
-#pragma unroll
-          for (int part = 0; part < 2; ++part) {             // the halves of P as they come
-            if (!ok || !wait_bar(p_full + 16 * s + 8 * part, (j - jb) & 1, abort_flag, a.err)) { ok = false; continue; }
+          };
+          if (!(ok = wait_one(q_full, n_q & 1))) break;
+          ++n_q;
+          const int head = min(step, w.je - w.jb);             // K tiles before the first V tile
+          for (int i = 0; i < head && ok; ++i) {
+            if (!(ok = wait_one(full0 + 8 * st, ph))) break;
             tc_fence_after();
 #pragma unroll
-            for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
-              if (kk < steps)
-                mma_bf16_ts(tmem + 2 * kTile + s * HD, tmem + s * kTile + kk * 8, bd + kk * (2048 >> 4), idesc_o,
-                            j > jb || kk > 0);
+            for (int s = 0; s < 2; ++s)
+              if (active(s, w.jb + i)) scores(s, w.jb + i, st);
+            mma_commit(empty0 + 8 * st);
+            advance();
           }
-          if (!ok) continue;
-          if (j + 1 < je_s) {
-            if (!have_k) {
-              if (!wait_bar(full0 + 8 * st, ph, abort_flag, a.err)) { ok = false; continue; }
-              have_k = true;
-              tc_fence_after();
+          if (ok && w.jb + head == w.je) mma_commit(q_empty);  // every product that reads Q has been issued
+          for (int j = w.jb; j < w.je && ok; ++j) {
+            const uint32_t v_st = st;
+            if (!(ok = wait_one(full0 + 8 * st, ph))) break;
+            advance();
+            const uint32_t v_smem = kv_smem + v_st * Lay::kSlotBytes;
+            const int left = max(w.end[0], w.end[1]) - j * kTile;   // positions of this tile that any row sees
+            if (left < kTile && left % kPage) {
+              // the last page's rows beyond them hold anything (zero probabilities would not mask a NaN)
+              const int r0 = left, r1 = (left + kPage - 1) / kPage * kPage;
+              for (int i = 0; i < (r1 - r0) * 8 * kHalves; ++i) {
+                const int h = i / ((r1 - r0) * 8), x = i % ((r1 - r0) * 8);
+                *reinterpret_cast<uint4*>(smem + (v_smem - q_smem) + h * Lay::kHalf + r0 * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+              }
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
-            scores(s, j + 1, st);
+            tc_fence_after();
+            bool have_k = false;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              if (!ok || !active(s, j)) continue;
+              const int steps = min(kTile / kPage, ((s ? w.end[1] : w.end[0]) - j * kTile + kPage - 1) / kPage);
+              const uint64_t bd = sw128_mn_desc(v_smem, Lay::kHalf);
+              const uint32_t first_pv = j >= w.jb + step ? 1u : 0u;
+#pragma unroll
+              for (int part = 0; part < 2; ++part) {             // the halves of P as they come
+                if (!ok || !wait_one(p_full + 16 * s + 8 * part, n_p[s] & 1)) { ok = false; continue; }
+                tc_fence_after();
+#pragma unroll
+                for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
+                  if (kk < steps)
+                    mma_bf16_ts(tmem + 2 * kTile + s * HD, tmem + s * kTile + kk * 8, bd + kk * (2048 >> 4), idesc_o,
+                                kk > 0 ? 1u : first_pv);
+              }
+              if (!ok) continue;
+              ++n_p[s];
+              if (j + step < last[s]) {
+                if (!have_k) {
+                  if (!(ok = wait_one(full0 + 8 * st, ph))) continue;
+                  have_k = true;
+                  tc_fence_after();
+                }
+                scores(s, j + step, st);     // (its barrier also says that O has tile j)
+              } else {
+                mma_commit(o_full + 8 * s);
+              }
+            }
+            if (!ok) break;
+            mma_commit(empty0 + 8 * v_st);
+            if (have_k) {
+              mma_commit(empty0 + 8 * st);
+              advance();
+              if (j + step == w.je - 1) mma_commit(q_empty);
+            }
           }
-          mma_commit(s_full + 8 * s);      // S(j + 1) is there, O has tile j
         }
-        if (!ok) break;
-        mma_commit(empty0 + 8 * v_st);
-        if (have_k) {
-          mma_commit(empty0 + 8 * st);
-          advance();
-        }
+        mma_commit(drain);                   // all products issued by this thread have completed
+        wait_bar_budget(drain, 0, kDrainCycles);
       }
-      mma_commit(drain);                   // all products issued by this thread have completed
-      wait_bar_budget(drain, 0, kDrainCycles);
+      __syncwarp();
+    } else if (warp == 10) {
+      // Hands out the work: this block's own, then blocks that have not started (so that long and short
+      // pieces level out and one piece's prologue runs under the last one's products).
+      uint32_t n = 0, n_given = 0;
+      bool ok = true;
+      while (true) {
+        if (found) {
+          const uint32_t i = n & 1;
+          if (!(ok = wait_warp(w_empty + 8 * i, ((n >> 1) & 1) ^ 1))) break;
+          if (lane == 0) {
+            works[i] = first;
+            mbar_arrive(w_full + 8 * i);
+          }
+          __syncwarp();
+          ++n;
+          // no block is asked for before the loader has taken this piece
+          if (!(ok = wait_warp(w_taken, (n - 1) & 1))) break;
+        }
+        if (lane == 0) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the last answer has been read
+          mbar_expect_tx(given, 16);
+          request_block(smem_u32(&answer), given);
+        }
+        __syncwarp();
+        ++n_given;
+        if (!(ok = wait_warp(given, (n_given - 1) & 1))) break;
+        int x, y, z;
+        const bool more = read_block(smem_u32(&answer), x, y, z);
+        __syncwarp();
+        if (!more) break;
+        found = find_work(a, finder, x, y, z, first);
+      }
+      if (ok) {
+        const uint32_t i = n & 1;
+        if (wait_warp(w_empty + 8 * i, ((n >> 1) & 1) ^ 1) && lane == 0) {
+          works[i].seq = -1;
+          mbar_arrive(w_full + 8 * i);
+        }
+        __syncwarp();
+      } else if (n_given) {
+        wait_bar_budget(given, (n_given - 1) & 1, kDrainCycles);
+      }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int s = warp >> 2, r = (warp & 3) * 32 + lane;
     const int t = r / a.G, g = r - t * a.G;
-    const bool valid = t < (s ? sw.tokens[1] : sw.tokens[0]);
-    const int je_s = s ? je1 : je0;
-    const int see_r = valid ? min(sw.pos0 + s * a.T + t + 1, sw.kv) : 0;   // this row sees positions [0, see_r)
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + lanes + s * kTile, to = tmem + lanes + 2 * kTile + s * HD;
     const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD));   // scores in log2
-    float m = -INFINITY, l = 0.f;
+    uint32_t n_s = 0, n_o = 0;
     bool ok = true;
-    for (int j = jb; j < je_s; ++j) {
-      if (!wait_bar(s_full + 8 * s, (j - jb) & 1, abort_flag, a.err)) { ok = false; break; }
-      __syncwarp();
+    while (ok) {
+      int j0, je_s, step, see_r, split, solo;
+      size_t item;
+      bool valid;
+      {
+        Work w;
+        if (!next_work(w, wait_warp)) break;
+        const int from = w.solo ? 0 : s * a.T;
+        solo = w.solo;
+        step = 1 + w.solo;
+        j0 = w.jb + (w.solo ? s : 0);
+        je_s = s ? last_tile(w, 1) : last_tile(w, 0);
+        valid = t < (s ? w.tokens[1] : w.tokens[0]);
+        see_r = valid ? min(w.pos0 + from + t + 1, w.kv) : 0;   // this row sees positions [0, see_r)
+        item = (static_cast<size_t>(w.row0) + from + t) * a.H + w.hk * a.G + g;
+        split = w.split;
+        __syncwarp();
+        if (lane == 0) done_reading();
+      }
+      float m = -INFINITY, l = 0.f;
+      for (int j = j0; j < je_s; j += step) {
+        if (!wait_warp(s_full + 8 * s, n_s & 1)) { ok = false; break; }
+        ++n_s;
+        tc_fence_after();
+        uint32_t x[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) ld32(ts + c * 32, x[c]);
+        ld_wait(x[0]);
+#pragma unroll
+        for (int c = 1; c < 4; ++c) ld_tie(x[c]);
+        const int vis = see_r - j * kTile;   // columns below vis are visible
+        if (vis < kTile) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (c * 32 + i >= vis) x[c][i] = 0xFF800000u;   // -inf
+        }
+        float top[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          top[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
+#pragma unroll
+          for (int i = 2; i < 32; i += 2) top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])));
+        }
+        float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        mx *= scale;
+        float f = 1.f;
+        if (mx > m + kGrowth || (m == -INFINITY && mx > m)) {
+          f = ex2(m - mx);
+          m = mx;
+          l *= f;
+        }
+        __syncwarp();
+        if (j > j0 && __any_sync(0xffffffffu, f != 1.f)) {
+#pragma unroll
+          for (int c = 0; c < HD / 32; ++c) {
+            uint32_t o[32];
+            ld32(to + c * 32, o);
+            ld_wait(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            st32(to + c * 32, o);
+          }
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        const uint64_t scale2 = pair(scale, scale), base2 = pair(-base, -base);
+        uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t p[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float e0, e1;
+            unpair(fma2(pair(__uint_as_float(x[c][2 * i]), __uint_as_float(x[c][2 * i + 1])), scale2, base2), e0, e1);
+            e0 = ex2(e0);
+            e1 = ex2(e1);
+            sum[i & 1] = add2(sum[i & 1], pair(e0, e1));
+            p[i] = pack_bf16(e0, e1);
+          }
+          st16(ts + c * 16, p);
+          if (c & 1) {                       // half of the tile's probabilities are there
+            st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * (c >> 1));
+          }
+        }
+        float s0, s1;
+        unpair(add2(sum[0], sum[1]), s0, s1);
+        l += s0 + s1;
+      }
+      if (je_s > j0 && ok) ok = wait_warp(o_full + 8 * s, n_o++ & 1);
+      if (!ok) break;
       tc_fence_after();
-      uint32_t x[4][32];
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const size_t n_items = static_cast<size_t>(a.M) * a.H;
+      const size_t part = (2 * static_cast<size_t>(split) + (solo ? s : 0)) * n_items + item;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) ld32(ts + c * 32, x[c]);
-      ld_wait(x[0]);
+      for (int c = 0; c < HD / 32; ++c) {
+        uint32_t o[32];
+        ld32(to + c * 32, o);
+        ld_wait(o);
 #pragma unroll
-      for (int c = 1; c < 4; ++c) ld_tie(x[c]);
-      const int vis = see_r - j * kTile;   // columns below vis are visible
-      if (vis < kTile) {
+        for (int i = 0; i < 32; ++i) o[i] = l > 0.f ? __float_as_uint(__uint_as_float(o[i]) * inv) : 0u;
+        if (valid) {
+          if (a.n_splits > 1) {
+            float* dst = a.part_o + part * HD + c * 32;
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+            for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(dst + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+          } else {
+            bf16* dst = a.out + item * HD + c * 32;
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (c * 32 + i >= vis) x[c][i] = 0xFF800000u;   // -inf
-      }
-      float top[4];
+            for (int i = 0; i < 32; i += 8) {
+              uint32_t v[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        top[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
-#pragma unroll
-        for (int i = 2; i < 32; i += 2) top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])));
-      }
-      float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-      mx *= scale;
-      float f = 1.f;
-      if (mx > m + kGrowth || (m == -INFINITY && mx > m)) {
-        f = ex2(m - mx);
-        m = mx;
-        l *= f;
-      }
-      __syncwarp();
-      if (j > jb && __any_sync(0xffffffffu, f != 1.f)) {
-#pragma unroll
-        for (int c = 0; c < HD / 32; ++c) {
-          uint32_t o[32];
-          ld32(to + c * 32, o);
-          ld_wait(o);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-          st32(to + c * 32, o);
-        }
-      }
-      const float base = m == -INFINITY ? 0.f : m;
-      const uint64_t scale2 = pair(scale, scale), base2 = pair(-base, -base);
-      uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t p[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float e0, e1;
-          unpair(fma2(pair(__uint_as_float(x[c][2 * i]), __uint_as_float(x[c][2 * i + 1])), scale2, base2), e0, e1);
-          e0 = ex2(e0);
-          e1 = ex2(e1);
-          sum[i & 1] = add2(sum[i & 1], pair(e0, e1));
-          p[i] = pack_bf16(e0, e1);
-        }
-        st16(ts + c * 16, p);
-        if (c & 1) {                       // half of the tile's probabilities are there
-          st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * (c >> 1));
-        }
-      }
-      float s0, s1;
-      unpair(add2(sum[0], sum[1]), s0, s1);
-      l += s0 + s1;
-    }
-    if (je_s > jb && ok) ok = wait_bar(s_full + 8 * s, (je_s - jb) & 1, abort_flag, a.err);
-    __syncwarp();
-    tc_fence_after();
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    const size_t item = (static_cast<size_t>(sw.row0) + s * a.T + t) * a.H + hk * a.G + g;
-    const size_t split = static_cast<size_t>(blockIdx.z) * a.M * a.H;
-#pragma unroll
-    for (int c = 0; c < HD / 32; ++c) {
-      uint32_t o[32];
-      ld32(to + c * 32, o);
-      ld_wait(o);
-#pragma unroll
-      for (int i = 0; i < 32; ++i) o[i] = l > 0.f ? __float_as_uint(__uint_as_float(o[i]) * inv) : 0u;
-      if (valid && ok) {
-        if (a.n_splits > 1) {
-          float* dst = a.part_o + (split + item) * HD + c * 32;
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(dst + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
-        } else {
-          bf16* dst = a.out + item * HD + c * 32;
-#pragma unroll
-          for (int i = 0; i < 32; i += 8) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              w[e] = pack_bf16(__uint_as_float(o[i + 2 * e]), __uint_as_float(o[i + 2 * e + 1]));
-            *reinterpret_cast<uint4*>(dst + i) = make_uint4(w[0], w[1], w[2], w[3]);
+              for (int e = 0; e < 4; ++e)
+                v[e] = pack_bf16(__uint_as_float(o[i + 2 * e]), __uint_as_float(o[i + 2 * e + 1]));
+              *reinterpret_cast<uint4*>(dst + i) = make_uint4(v[0], v[1], v[2], v[3]);
+            }
           }
         }
       }
-    }
-    if (valid && ok) {
-      const float l2 = l > 0.f ? m + log2f(l) : -INFINITY;
-      if (a.n_splits > 1) a.part_lse[split + item] = l2;
-      else if (a.lse) a.lse[item] = l2 * 0.6931471805599453f;
+      if (valid) {
+        const float l2 = l > 0.f ? m + log2f(l) : -INFINITY;
+        if (a.n_splits > 1) {
+          a.part_lse[part] = l2;
+          if (!solo) a.part_lse[part + n_items] = -INFINITY;   // no second half
+        } else if (a.lse) {
+          a.lse[item] = l2 * 0.6931471805599453f;
+        }
+      }
     }
   }
   tc_fence_before();
@@ -528,13 +680,15 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant_
   const size_t item = static_cast<size_t>(blockIdx.x) * 4 + (threadIdx.x >> 5), n = static_cast<size_t>(a.M) * a.H;
   if (item >= n || static_cast<int>(item / a.H) >= a.cu[a.n_seq]) return;
   float mx = -INFINITY;
-  for (int z = lane; z < a.n_splits; z += 32) mx = fmaxf(mx, a.part_lse[z * n + item]);
+  const int parts = 2 * a.n_splits;
+  for (int z = lane; z < parts; z += 32) mx = fmaxf(mx, a.part_lse[z * n + item]);
   mx = warp_max(mx);
   const float base = mx == -INFINITY ? 0.f : mx;
   constexpr int kPer = HD / 32;
   float acc[kPer] = {}, total = 0.f;
-  for (int z = 0; z < a.n_splits; ++z) {
+  for (int z = 0; z < parts; ++z) {
     const float w = ex2(a.part_lse[z * n + item] - base);
+    if (w == 0.f) continue;                // nothing seen there (or nothing written)
     total += w;
     const float* o = a.part_o + (z * n + item) * HD + lane * kPer;
 #pragma unroll
@@ -590,7 +744,7 @@ using namespace sd2;
 size_t sd2_attention_prompt_workspace_bytes(int32_t M, int32_t n_seq, int32_t H, int32_t Hkv, int32_t hd, int32_t max_kv) {
   if (M < 1 || n_seq < 1 || Hkv < 1 || H < Hkv || H % Hkv || (hd != 64 && hd != 128) || max_kv < 1) return 0;
   const Shape s = shape_of(M, n_seq, H, Hkv, max_kv);
-  const size_t parts = s.splits > 1 ? static_cast<size_t>(s.splits) * M * H * (hd + 1) * 4 : 0;
+  const size_t parts = s.splits > 1 ? static_cast<size_t>(2 * s.splits) * M * H * (hd + 1) * 4 : 0;
   return 256 + (parts + 255) / 256 * 256;
 }
 
@@ -621,7 +775,7 @@ sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t
   // the workspace: a stand-in for the error word, then the splits' partial results
   a.err = d_err ? d_err : static_cast<unsigned*>(d_workspace);
   a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(d_workspace) + 256);
-  a.part_lse = a.part_o + static_cast<size_t>(s.splits) * M * H * hd;
+  a.part_lse = a.part_o + static_cast<size_t>(2 * s.splits) * M * H * hd;
   const bf16* pool = static_cast<const bf16*>(d_pool) + static_cast<size_t>(layer) * n_blocks * 2 * Hkv * kPage * hd;
   if (!encode_weight_map(&a.map_kv, pool, a.kv_rows, hd, kPage) ||
       !encode_rows_map(&a.map_q, d_q, hd, H, M, ldq, s.G, s.T))
