@@ -1291,16 +1291,15 @@ bool encode_weight_map(void* map, const void* w, int rows, int K, int box_rows) 
   return make_map(static_cast<CUtensorMap*>(map), w, rows, K, K, box_rows);
 }
 
-bool encode_rows_map(void* map, const void* base, int hd, int heads, long long rows, long long ld, int box_heads,
-                     int box_rows) {
+bool encode_map3(void* map, const void* base, const Dims3& dims, const Strides2& strides, const Dims3& box) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(hd) * 2, static_cast<cuuint64_t>(ld) * 2};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_heads), static_cast<cuuint32_t>(box_rows)};
+  const cuuint64_t d[3] = {static_cast<cuuint64_t>(dims.x), static_cast<cuuint64_t>(dims.y), static_cast<cuuint64_t>(dims.z)};
+  const cuuint64_t st[2] = {static_cast<cuuint64_t>(strides.y) * 2, static_cast<cuuint64_t>(strides.z) * 2};
+  const cuuint32_t b[3] = {static_cast<cuuint32_t>(box.x), static_cast<cuuint32_t>(box.y), static_cast<cuuint32_t>(box.z)};
   const cuuint32_t estr[3] = {1, 1, 1};
-  return fn(static_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides,
-            box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+  return fn(static_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), d, st, b, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

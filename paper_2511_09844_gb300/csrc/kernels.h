@@ -142,10 +142,15 @@ cudaError_t gemm_simt(const GemmArgs& a, cudaStream_t st);
 // 2-D bf16 TMA map (CUtensorMap, 128 bytes) of a row-major [rows, K] weight: boxes of box_rows x 64
 // elements with the 128-byte swizzle (gemm_tc.cu).
 bool encode_weight_map(void* map, const void* w, int rows, int K, int box_rows);
-// 3-D bf16 TMA map of packed rows [rows][heads][hd] with row stride ld (elements): boxes of box_rows rows
-// x box_heads heads x 64 elements with the 128-byte swizzle (gemm_tc.cu).
-bool encode_rows_map(void* map, const void* base, int hd, int heads, long long rows, long long ld, int box_heads,
-                     int box_rows);
+// 3-D bf16 TMA map with the 128-byte swizzle (gemm_tc.cu): extents, the strides of y and z in elements
+// (multiples of 8), and the box, 64 elements wide.
+struct Dims3 {
+  long long x, y, z;
+};
+struct Strides2 {
+  long long y, z;
+};
+bool encode_map3(void* map, const void* base, const Dims3& dims, const Strides2& strides, const Dims3& box);
 int sm_count_cached();
 
 // ---------------------------------------------------------------- decoder elementwise

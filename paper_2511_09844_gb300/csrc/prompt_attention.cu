@@ -26,6 +26,8 @@
 #include "kernels.h"
 #include "tc.cuh"
 
+#include <limits.h>
+
 #include <algorithm>
 #include <string>
 
@@ -43,11 +45,12 @@ constexpr int kMaxStages = 8;
 constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum that makes O be rescaled
 
 struct PromptArgs {
-  CUtensorMap map_q, map_kv;
+  CUtensorMap map_q, map_k, map_v;
   int M, H, Hkv, G, T;                     // G heads per KV head, T tokens per slot
   int n_blocks, bt_stride, n_seq, n_splits;
-  int kv_rows;                             // rows of map_kv
+  int kv_rows;                             // rows of map_k and map_v
   const int *table, *cu, *kv_len;
+  const bf16* pool;                        // the layer's pages
   bf16* out;
   float* lse;
   float *part_o, *part_lse;                // [2 n_splits][M * H][hd] and [2 n_splits][M * H] (log2)
@@ -57,9 +60,15 @@ struct PromptArgs {
 template <int HD>
 struct Layout {
   static constexpr int kSlotBytes = kTile * HD * 2;     // a query tile, or a K or V tile
-  static constexpr int kHalf = kTile * 128;             // its 64-column half
-  static constexpr int kStages = HD == 128 ? 5 : 8;
-  static constexpr int kBytes = (2 + kStages) * kSlotBytes;
+  static constexpr int kHalf = kTile * 128;             // its 64-column half (of Q and K; V lies page by page)
+  static constexpr int kPageBytes = kPage * HD * 2;
+  static constexpr int kStages = HD == 128 ? 4 : 8;
+  static constexpr int kStaging = 8 * 4096;             // a 4 KB panel per softmax warp for the results' way out
+  static constexpr int kBytes = (2 + kStages) * kSlotBytes + kStaging;
+  // TMEM columns: S of each slot, then O, then P: over S where TMEM is full (hd 128)
+  static constexpr int kO = 2 * kTile, kP = HD == 128 ? 0 : 2 * kTile + 2 * HD, kPStride = HD == 128 ? kTile : kTile / 2;
+  // P apart from S: the next scores are computed while the softmax of the current ones runs
+  static constexpr bool kEarly = HD != 128;
   static constexpr int kSmem = kBytes + 1024 + 256;     // + alignment + barriers
 };
 
@@ -163,6 +172,28 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&t);
 }
 
+// Bounded wait of the MMA thread: polls (a suspended wait wakes up some hundred cycles late).
+__device__ __forceinline__ bool wait_spin(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned* err) {
+  const long long t0 = clock64();
+  for (uint32_t it = 1;; ++it) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((it & 63) == 0) {
+      if (*abort_flag) return false;
+      if (clock64() - t0 > kWaitCycles) {
+        *abort_flag = 1;
+        atomicOr(err, static_cast<unsigned>(ERR_TIMEOUT));
+        return false;
+      }
+    }
+  }
+}
+
 // True in one thread of the (converged) warp: the compiler then knows that the code under it runs in a single
 // thread and keeps the MMA operands in uniform registers (under a lane == 0 test each MMA took 125 cycles to
 // issue, more than it runs).
@@ -172,60 +203,90 @@ __device__ __forceinline__ bool elect_one() {
   return p != 0;
 }
 
-// Finds tile `tile` of the grid (one warp): tiles are numbered through the sequences, the last of each first
-// (it sees the most positions). The first 32 sequences stay in the lanes' registers.
-struct Finder {
-  int lo, hi, len, n, sum;                 // this lane's sequence: packed rows, cached length, tiles; inclusive sum of n
+// The sequence of each lane (one warp holds up to 32 of them).
+struct Seqs {
+  int lo, rows, len, n;                    // first packed row, rows, cached length, tiles of 2 T rows
   __device__ __forceinline__ void load(const PromptArgs& a, int s) {
-    lo = hi = len = 0;
+    lo = rows = len = 0;
     if (s < a.n_seq) {
       lo = min(max(a.cu[s], 0), a.M);
-      hi = min(max(a.cu[s + 1], lo), a.M);
-      len = a.kv_len[s];
+      rows = min(max(a.cu[s + 1], lo), a.M) - lo;
+      len = min(a.kv_len[s], 1 << 30);
     }
-    n = (hi - lo + 2 * a.T - 1) / (2 * a.T);
-    sum = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int t = __shfl_up_sync(0xffffffffu, sum, o);
-      if ((threadIdx.x & 31) >= o) sum += t;
-    }
+    n = (rows + 2 * a.T - 1) / (2 * a.T);
+  }
+  // tiles whose rows see more than e positions (the last ones)
+  __device__ __forceinline__ int longer(int per, int e) const {
+    return e >= len ? 0 : n - min(max((e - (len - rows)) / per, 0), n);
   }
 };
-__device__ bool find_work(const PromptArgs& a, const Finder& first, int tile, int hk, int split, Work& w) {
-  const int lane = threadIdx.x & 31, per = 2 * a.T;
-  Finder f = first;
-  int before = 0;
-  for (int s0 = 0; s0 < a.n_seq; s0 += 32) {
-    if (s0) f.load(a, s0 + lane);
-    const unsigned hit = __ballot_sync(0xffffffffu, before + f.sum > tile);
-    if (hit) {
-      const int src = __ffs(hit) - 1;
-      const int n_s = __shfl_sync(0xffffffffu, f.n, src), end_s = before + __shfl_sync(0xffffffffu, f.sum, src);
-      const int lo_s = __shfl_sync(0xffffffffu, f.lo, src), hi_s = __shfl_sync(0xffffffffu, f.hi, src);
-      const int len = __shfl_sync(0xffffffffu, f.len, src);
-      const int t = n_s - 1 - (tile - (end_s - n_s)), rows = hi_s - lo_s;
-      w.seq = s0 + src;
-      w.hk = hk;
-      w.split = split;
-      w.row0 = lo_s + t * per;
-      w.pos0 = len - rows + t * per;
-      w.kv = min(max(len, 0), a.bt_stride * kPage);
-      w.solo = a.n_splits > 1 && rows - t * per <= a.T;
+__device__ __forceinline__ int warp_scan(int v) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int from = w.solo ? 0 : i * a.T;
-        w.tokens[i] = min(max(rows - t * per - from, 0), a.T);
-        w.end[i] = w.tokens[i] ? min(max(w.pos0 + from + w.tokens[i], 0), w.kv) : 0;
-      }
-      const long long nt = (max(w.end[0], w.end[1]) + kTile - 1) / kTile;
-      w.jb = static_cast<int>(nt * split / a.n_splits);
-      w.je = static_cast<int>(nt * (split + 1) / a.n_splits);
-      return true;
-    }
-    before += __shfl_sync(0xffffffffu, f.sum, 31);
+  for (int o = 1; o < 32; o <<= 1) {
+    const int t = __shfl_up_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) >= o) v += t;
   }
-  return false;
+  return v;
+}
+
+// Finds tile `tile` of the grid (one warp). Up to 32 sequences: tiles are numbered by the K/V tiles that they
+// walk, the longest first, so that the short ones fill the end of the grid. More sequences: through the
+// sequences, each from its last (longest) tile.
+__device__ bool find_work(const PromptArgs& a, const Seqs& first, int tile, int hk, int split, Work& w) {
+  const int lane = threadIdx.x & 31, per = 2 * a.T;
+  Seqs f = first;
+  int s0 = 0, src = -1, t = 0;
+  if (a.n_seq <= 32) {
+    if (tile >= __reduce_add_sync(0xffffffffu, f.n)) return false;
+    // the largest e with more than `tile` tiles that walk at least e K/V tiles
+    int e = 0, top = 1 + (__reduce_max_sync(0xffffffffu, max(f.len, 0)) + kTile - 1) / kTile;
+    if (a.n_seq == 1) {
+      src = 0;
+      t = __shfl_sync(0xffffffffu, f.n, 0) - 1 - tile;
+    } else {
+      while (top - e > 1) {
+        const int mid = (e + top) / 2;
+        if (static_cast<int>(__reduce_add_sync(0xffffffffu, f.longer(per, (mid - 1) * kTile))) > tile) e = mid; else top = mid;
+      }
+      const int at_least = e ? f.longer(per, (e - 1) * kTile) : f.n, more = f.longer(per, e * kTile);
+      const int rank = tile - __reduce_add_sync(0xffffffffu, more);
+      const int sum = warp_scan(at_least - more);
+      src = __ffs(__ballot_sync(0xffffffffu, sum > rank)) - 1;
+      t = __shfl_sync(0xffffffffu, f.n - 1 - more - (rank - (sum - (at_least - more))), src);
+    }
+  } else {
+    for (int before = 0; s0 < a.n_seq; s0 += 32) {
+      if (s0) f.load(a, s0 + lane);
+      const int sum = before + warp_scan(f.n);
+      const unsigned hit = __ballot_sync(0xffffffffu, sum > tile);
+      if (hit) {
+        src = __ffs(hit) - 1;
+        t = __shfl_sync(0xffffffffu, sum - 1 - tile, src);
+        break;
+      }
+      before = __shfl_sync(0xffffffffu, sum, 31);
+    }
+    if (src < 0) return false;
+  }
+  const int lo = __shfl_sync(0xffffffffu, f.lo, src), rows = __shfl_sync(0xffffffffu, f.rows, src);
+  const int len = __shfl_sync(0xffffffffu, f.len, src);
+  w.seq = s0 + src;
+  w.hk = hk;
+  w.split = split;
+  w.row0 = lo + t * per;
+  w.pos0 = len - rows + t * per;
+  w.kv = min(max(len, 0), a.bt_stride * kPage);
+  w.solo = a.n_splits > 1 && rows - t * per <= a.T;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int from = w.solo ? 0 : i * a.T;
+    w.tokens[i] = min(max(rows - t * per - from, 0), a.T);
+    w.end[i] = w.tokens[i] ? min(max(w.pos0 + from + w.tokens[i], 0), w.kv) : 0;
+  }
+  const long long nt = (max(w.end[0], w.end[1]) + kTile - 1) / kTile;
+  w.jb = static_cast<int>(nt * split / a.n_splits);
+  w.je = static_cast<int>(nt * (split + 1) / a.n_splits);
+  return true;
 }
 
 // Cluster launch control: asks for a block of this grid that has not started yet; the answer (16 bytes)
@@ -249,7 +310,7 @@ __device__ __forceinline__ bool read_block(uint32_t answer, int& x, int& y, int&
   return ok != 0;
 }
 
-constexpr int kConsumers = 10;             // of a piece of work: the loader, the MMA thread, 8 softmax warps
+constexpr int kConsumers = 11;             // of a piece of work: two loaders, the MMA thread, 8 softmax warps
 
 template <int HD>
 __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __grid_constant__ PromptArgs a) {
@@ -259,27 +320,31 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   __shared__ Work works[2];
   __shared__ __align__(16) uint4 answer;
-  __shared__ int flags[2];                 // [0] abort, [1] TMEM base
-  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 16];
+  __shared__ int flags[3];                 // [0] abort, [1] TMEM base, [2] the block has work of its own
+  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 20];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * S, q_full = empty0 + 8 * S, q_empty = q_full + 8,
-                 s_full = q_empty + 8, o_full = s_full + 16, p_full = o_full + 16, drain = p_full + 32,
+                 s_full = q_empty + 8, s_free = s_full + 16, o_full = s_free + 16, p_full = o_full + 16, drain = p_full + 32,
                  w_full = drain + 8, w_empty = w_full + 16, w_taken = w_empty + 16, given = w_taken + 8;
   const uint32_t q_smem = smem_u32(smem), kv_smem = q_smem + 2 * Lay::kSlotBytes;
   volatile int* abort_flag = flags;
   if (a.n_splits > 1) pdl_trigger();       // the join may be set up (it waits for this grid to complete)
   Work first{};
-  Finder finder{};
+  Seqs finder{};
   bool found = false;
   if (warp == 10) {
     finder.load(a, lane);
-    found = find_work(a, finder, blockIdx.x, blockIdx.y, blockIdx.z, first);
+    found = find_work(a, finder, blockIdx.y, blockIdx.x, blockIdx.z, first);
+    if (lane == 0) {
+      works[0] = first;
+      flags[2] = found;
+    }
   } else if (warp == 9) {
     tmem_alloc(smem_u32(&flags[1]), 512);
     tmem_relinquish();
   } else if (warp == 8) {
-    if (lane < 2)
-      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &a.map_q : &a.map_kv)) : "memory");
+    if (lane < 3)
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&a.map_q + lane)) : "memory");
   } else if (threadIdx.x == 0) {
     flags[0] = 0;
     for (int i = 0; i < S; ++i) {
@@ -290,6 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
     mbar_init(q_empty, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + 8 * i, 1);
+      mbar_init(s_free + 8 * i, 4);
       mbar_init(o_full + 8 * i, 1);
       mbar_init(p_full + 16 * i, 4);
       mbar_init(p_full + 16 * i + 8, 4);
@@ -311,7 +377,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
   uint32_t n_work = 0;
   auto next_work = [&](Work& w, auto wait) {
     const uint32_t i = n_work & 1;
-    if (!wait(w_full + 8 * i, (n_work >> 1) & 1)) return false;
+    // (the block's own piece is there since the first barrier)
+    if ((n_work || !flags[2]) && !wait(w_full + 8 * i, (n_work >> 1) & 1)) return false;
     w = works[i];
     ++n_work;
     return w.seq >= 0;
@@ -322,48 +389,78 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == 8) {
+    if (warp == 8 || warp == 11) {
+      // Warp 8 loads Q and the K tiles, warp 11 the V tiles; both walk the same sequence of ring stages. A page of
+      // one head is contiguous, so V takes one copy per page (its halves behind each other: the products take 16
+      // positions at a time); K, whose tile one product reads whole, takes one per page and half. A lane issues each:
+      // by one thread they take 150 cycles a copy, by one warp for both more than the products.
+      const int v_warp = warp == 11;
       Work w;
-      const int page = lane / kHalves, half = lane % kHalves;
       uint32_t u = 0, st = 0, ph = 0, n_q = 0;
       bool ok = true;
       while (ok && next_work(w, wait_warp)) {
         __syncwarp();
         if (lane == 0) {
           done_reading();
-          mbar_arrive(w_taken);
+          if (!v_warp) mbar_arrive(w_taken);
         }
         if (w.jb >= w.je) continue;
         const int* row = a.table + static_cast<size_t>(w.seq) * a.bt_stride;
         const int see = max(w.end[0], w.end[1]), n_pages = (see + kPage - 1) / kPage, step = 1 + w.solo;
+        const int page = v_warp ? lane : lane / kHalves, half = v_warp ? 0 : lane % kHalves;   // this lane's copy
         auto id_of = [&](int j) {
           const int i = j * (kTile / kPage) + page;
           return j < w.je && page < kTile / kPage && i < n_pages ? row[i] : 0;
         };
-        int id[3];                           // page ids of tiles j, j + 1, j + 2
+        int id[3];                           // of tiles j, j + 1, j + 2
         id[0] = id_of(w.jb);
         id[1] = id_of(w.jb + 1);
-        // Q once the last piece's scores are done
-        if (!(ok = wait_warp(q_empty, (n_q & 1) ^ 1))) break;
-        if (lane == 0) {
+        if (!v_warp) {
+          // Q once the last piece's scores are done
+          if (!(ok = wait_warp(q_empty, (n_q & 1) ^ 1))) break;
           const int slots = !w.solo && last_tile(w, 0) > w.jb && last_tile(w, 1) > w.jb ? 2 : 1;
-          const int s0 = !w.solo && last_tile(w, 0) <= w.jb ? 1 : 0;
-          mbar_expect_tx(q_full, static_cast<uint32_t>(slots * kHalves * a.T * a.G * 128));
-          for (int s = s0; s < s0 + slots; ++s)
-            for (int h = 0; h < kHalves; ++h)
-              tma_load_3d(q_smem + s * Lay::kSlotBytes + h * Lay::kHalf, &a.map_q, h * 64, w.hk * a.G, w.row0 + s * a.T, q_full);
-        }
-        ++n_q;
-        auto load = [&](int j, int v, int page_id) {
-          const int np = min(kTile / kPage, n_pages - j * (kTile / kPage));
-          const bool bad = page_id < 0 || page_id >= a.n_blocks;
-          if (bad && page < np && a.err) atomicOr(a.err, static_cast<unsigned>(ERR_RANGE));
-          if (!wait_warp(empty0 + 8 * st, ph ^ 1)) return false;
-          if (lane == 0) mbar_expect_tx(full0 + 8 * st, static_cast<uint32_t>(np * kPage * HD * 2));
+          if (lane == 0) mbar_expect_tx(q_full, static_cast<uint32_t>(slots * kHalves * a.T * a.G * 128));
           __syncwarp();
-          if (page < np)                     // a page that does not exist lies outside the map: zeros
-            tma_load_2d(kv_smem + st * Lay::kSlotBytes + half * Lay::kHalf + page * (kPage * 128), &a.map_kv, half * 64,
-                        bad ? a.kv_rows : ((page_id * 2 + v) * a.Hkv + w.hk) * kPage, full0 + 8 * st);
+          const int s = lane / kHalves + (!w.solo && last_tile(w, 0) <= w.jb ? 1 : 0);
+          if (lane < slots * kHalves)
+            tma_load_3d(q_smem + s * Lay::kSlotBytes + half * Lay::kHalf, &a.map_q, half * 64, w.hk * a.G, w.row0 + s * a.T, q_full);
+          ++n_q;
+        }
+        auto load = [&](int j, int v, int page_id) {
+          if (v == v_warp) {
+            int np = min(kTile / kPage, n_pages - j * (kTile / kPage));
+            bool bad = page_id < 0 || page_id >= a.n_blocks;
+            if (bad && page < np && a.err) atomicOr(a.err, static_cast<unsigned>(ERR_RANGE));
+            if (!wait_warp(empty0 + 8 * st, ph ^ 1)) return false;
+            const uint32_t dst = kv_smem + st * Lay::kSlotBytes;
+            // a page that does not exist lies outside the map: zeros
+            const int at = bad ? a.kv_rows : ((page_id * 2 + v) * a.Hkv + w.hk) * kPage;
+            const int rows = w.kv - (j * kTile + (np - 1) * kPage);   // of the last page, that exist
+            if (v && rows < kPage) {
+              // Rows beyond the cached length hold anything, and a zero probability would not mask a NaN there: this
+              // page comes through registers, those rows as zeros.
+              --np;
+              const int src = __shfl_sync(0xffffffffu, at, np);
+              const bool none = __shfl_sync(0xffffffffu, static_cast<int>(bad), np);
+#pragma unroll 1
+              for (int i = lane; i < kPage * 8 * kHalves; i += 32) {
+                const int r = i / (8 * kHalves), c = i % (8 * kHalves);
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (r < rows && !none)
+                  x = *reinterpret_cast<const uint4*>(a.pool + (static_cast<size_t>(src) + r) * HD + c * 8);
+                *reinterpret_cast<uint4*>(smem + (dst - q_smem) + np * Lay::kPageBytes + (c / 8) * (kPage * 128) + r * 128 +
+                                          ((c % 8) ^ (r & 7)) * 16) = x;
+              }
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+            }
+            if (lane == 0) mbar_expect_tx(full0 + 8 * st, static_cast<uint32_t>(np * Lay::kPageBytes));
+            __syncwarp();
+            if (page < np) {
+              if (v_warp) tma_load_3d(dst + page * Lay::kPageBytes, &a.map_v, 0, at, 0, full0 + 8 * st);
+              else tma_load_3d(dst + half * Lay::kHalf + page * (kPage * 128), &a.map_k, half * 64, at, 0, full0 + 8 * st);
+            }
+          }
           if (++st == S) { st = 0; ph ^= 1u; }
           ++u;
           return true;
@@ -372,8 +469,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         if (ok && step == 2 && w.jb + 1 < w.je) ok = load(w.jb + 1, 0, id[1]);
         for (int j = w.jb; j < w.je && ok; ++j) {
           id[2] = id_of(j + 2);
-          ok = load(j, 1, id[0]);
+          if (!Lay::kEarly) ok = load(j, 1, id[0]);
           if (ok && j + step < w.je) ok = load(j + step, 0, step == 2 ? id[2] : id[1]);
+          if (Lay::kEarly && ok) ok = load(j, 1, id[0]);
           id[0] = id[1];
           id[1] = id[2];
         }
@@ -385,19 +483,26 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       }
     } else if (warp == 9) {
       if (elect_one()) {
+        auto wait = [&](uint32_t bar, uint32_t parity) { return wait_spin(bar, parity, abort_flag, a.err); };
         const uint32_t idesc_s = idesc_bf16(kTile, 0), idesc_o = idesc_bf16(kTile, HD) | (1u << 16);   // B of P V is MN-major
         const uint64_t q_desc = sw128_desc(q_smem);
         Work w;
         bool ok = true;
-        uint32_t st = 0, ph = 0, n_q = 0, n_p[2] = {0, 0};     // ring position of the next tile, Q tiles, P tiles so far
+        uint32_t st = 0, ph = 0, n_q = 0;                      // ring position of the next tile, Q tiles so far
+        uint32_t n_p[2] = {0, 0}, n_sc[2] = {0, 0};            // P and S tiles so far
         auto advance = [&]() { if (++st == S) { st = 0; ph ^= 1u; } };
-        while (ok && next_work(w, wait_one)) {
+        while (ok && next_work(w, wait)) {
           done_reading();
           if (w.jb >= w.je) continue;
           const int step = 1 + w.solo;
           const int last[2] = {last_tile(w, 0), last_tile(w, 1)};
           auto active = [&](int s, int j) { return j < last[s] && (!w.solo || ((j - w.jb) & 1) == s); };
           auto scores = [&](int s, int j, uint32_t k_st) {     // S_s = Q_s K_j^T over the pages that the slot sees
+            if (Lay::kEarly) {                                 // the softmax has taken the last scores
+              if (!wait(s_free + 8 * s, (n_sc[s] & 1) ^ 1)) { ok = false; return; }
+              tc_fence_after();
+            }
+            ++n_sc[s];
             const int n = min(kTile, ((s ? w.end[1] : w.end[0]) - j * kTile + kPage - 1) / kPage * kPage);
             const uint32_t id = idesc_s | (static_cast<uint32_t>(n >> 3) << 17);
             const uint64_t ad = q_desc + (w.solo ? 0 : (s * Lay::kSlotBytes) >> 4), bd = sw128_desc(kv_smem + k_st * Lay::kSlotBytes);
@@ -408,72 +513,75 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
             }
             mma_commit(s_full + 8 * s);
           };
-          if (!(ok = wait_one(q_full, n_q & 1))) break;
+          auto values = [&](int s, int j, uint32_t v_smem) {   // O_s += P_s V_j, the halves of P as they come
+            const int steps = min(kTile / kPage, ((s ? w.end[1] : w.end[0]) - j * kTile + kPage - 1) / kPage);
+            const uint64_t bd = sw128_mn_desc(v_smem, kPage * 128);
+            const uint32_t more = j >= w.jb + step ? 1u : 0u;
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+              if (!ok || !wait(p_full + 16 * s + 8 * part, n_p[s] & 1)) { ok = false; continue; }
+              tc_fence_after();
+#pragma unroll
+              for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
+                if (kk < steps)
+                  mma_bf16_ts(tmem + Lay::kO + s * HD, tmem + Lay::kP + s * Lay::kPStride + kk * 8,
+                              bd + kk * (Lay::kPageBytes >> 4), idesc_o, kk > 0 ? 1u : more);
+            }
+            ++n_p[s];
+            // O has tile j (where the next scores follow P in its columns, their barrier says so too)
+            if (ok && (Lay::kEarly || j + step >= last[s])) mma_commit(o_full + 8 * s);
+          };
+          if (!(ok = wait(q_full, n_q & 1))) break;
           ++n_q;
           const int head = min(step, w.je - w.jb);             // K tiles before the first V tile
           for (int i = 0; i < head && ok; ++i) {
-            if (!(ok = wait_one(full0 + 8 * st, ph))) break;
+            if (!(ok = wait(full0 + 8 * st, ph))) break;
             tc_fence_after();
 #pragma unroll
             for (int s = 0; s < 2; ++s)
-              if (active(s, w.jb + i)) scores(s, w.jb + i, st);
+              if (ok && active(s, w.jb + i)) scores(s, w.jb + i, st);
             mma_commit(empty0 + 8 * st);
             advance();
           }
           if (ok && w.jb + head == w.je) mma_commit(q_empty);  // every product that reads Q has been issued
           for (int j = w.jb; j < w.je && ok; ++j) {
-            const uint32_t v_st = st;
-            if (!(ok = wait_one(full0 + 8 * st, ph))) break;
-            advance();
-            const uint32_t v_smem = kv_smem + v_st * Lay::kSlotBytes;
-            const int left = max(w.end[0], w.end[1]) - j * kTile;   // positions of this tile that any row sees
-            if (left < kTile && left % kPage) {
-              // the last page's rows beyond them hold anything (zero probabilities would not mask a NaN)
-              const int r0 = left, r1 = (left + kPage - 1) / kPage * kPage;
-              for (int i = 0; i < (r1 - r0) * 8 * kHalves; ++i) {
-                const int h = i / ((r1 - r0) * 8), x = i % ((r1 - r0) * 8);
-                *reinterpret_cast<uint4*>(smem + (v_smem - q_smem) + h * Lay::kHalf + r0 * 128 + x * 16) = make_uint4(0, 0, 0, 0);
-              }
-              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            }
-            tc_fence_after();
-            bool have_k = false;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              if (!ok || !active(s, j)) continue;
-              const int steps = min(kTile / kPage, ((s ? w.end[1] : w.end[0]) - j * kTile + kPage - 1) / kPage);
-              const uint64_t bd = sw128_mn_desc(v_smem, Lay::kHalf);
-              const uint32_t first_pv = j >= w.jb + step ? 1u : 0u;
-#pragma unroll
-              for (int part = 0; part < 2; ++part) {             // the halves of P as they come
-                if (!ok || !wait_one(p_full + 16 * s + 8 * part, n_p[s] & 1)) { ok = false; continue; }
-                tc_fence_after();
-#pragma unroll
-                for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
-                  if (kk < steps)
-                    mma_bf16_ts(tmem + 2 * kTile + s * HD, tmem + s * kTile + kk * 8, bd + kk * (2048 >> 4), idesc_o,
-                                kk > 0 ? 1u : first_pv);
-              }
-              if (!ok) continue;
-              ++n_p[s];
-              if (j + step < last[s]) {
-                if (!have_k) {
-                  if (!(ok = wait_one(full0 + 8 * st, ph))) continue;
-                  have_k = true;
-                  tc_fence_after();
-                }
-                scores(s, j + step, st);     // (its barrier also says that O has tile j)
-              } else {
-                mma_commit(o_full + 8 * s);
-              }
-            }
-            if (!ok) break;
-            mma_commit(empty0 + 8 * v_st);
-            if (have_k) {
-              mma_commit(empty0 + 8 * st);
+            const bool k_next = j + step < w.je;
+            uint32_t k_st = 0, v_st = 0;
+            auto take = [&](uint32_t& x) {                     // the next tile of the ring
+              x = st;
+              if (!wait(full0 + 8 * st, ph)) { ok = false; return; }
               advance();
-              if (j + step == w.je - 1) mma_commit(q_empty);
+              tc_fence_after();
+            };
+            if (Lay::kEarly) {
+              if (k_next) {
+                take(k_st);
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+                  if (ok && active(s, j) && j + step < last[s]) scores(s, j + step, k_st);
+                if (ok) mma_commit(empty0 + 8 * k_st);
+              }
+              if (ok) take(v_st);
+#pragma unroll
+              for (int s = 0; s < 2; ++s)
+                if (ok && active(s, j)) values(s, j, kv_smem + v_st * Lay::kSlotBytes);
+              if (ok) mma_commit(empty0 + 8 * v_st);
+            } else {
+              bool have_k = false;
+              take(v_st);
+#pragma unroll
+              for (int s = 0; s < 2; ++s) {
+                if (!ok || !active(s, j)) continue;
+                values(s, j, kv_smem + v_st * Lay::kSlotBytes);
+                if (!ok || j + step >= last[s]) continue;
+                if (!have_k) take(k_st);
+                have_k = true;
+                if (ok) scores(s, j + step, k_st);
+              }
+              if (ok) mma_commit(empty0 + 8 * v_st);
+              if (ok && have_k) mma_commit(empty0 + 8 * k_st);
             }
+            if (ok && j + step == w.je - 1) mma_commit(q_empty);
           }
         }
         mma_commit(drain);                   // all products issued by this thread have completed
@@ -490,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           const uint32_t i = n & 1;
           if (!(ok = wait_warp(w_empty + 8 * i, ((n >> 1) & 1) ^ 1))) break;
           if (lane == 0) {
-            works[i] = first;
+            if (n || !flags[2]) works[i] = first;   // (the block's own piece is there already)
             mbar_arrive(w_full + 8 * i);
           }
           __syncwarp();
@@ -510,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         const bool more = read_block(smem_u32(&answer), x, y, z);
         __syncwarp();
         if (!more) break;
-        found = find_work(a, finder, x, y, z, first);
+        found = find_work(a, finder, y, x, z, first);
       }
       if (ok) {
         const uint32_t i = n & 1;
@@ -528,7 +636,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
     const int s = warp >> 2, r = (warp & 3) * 32 + lane;
     const int t = r / a.G, g = r - t * a.G;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + lanes + s * kTile, to = tmem + lanes + 2 * kTile + s * HD;
+    const uint32_t ts = tmem + lanes + s * kTile, to = tmem + lanes + Lay::kO + s * HD;
+    const uint32_t tp = tmem + lanes + Lay::kP + s * Lay::kPStride;
+    unsigned char* panel = smem + (2 + S) * Lay::kSlotBytes + warp * 4096;
     const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD));   // scores in log2
     uint32_t n_s = 0, n_o = 0;
     bool ok = true;
@@ -545,7 +655,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         j0 = w.jb + (w.solo ? s : 0);
         je_s = s ? last_tile(w, 1) : last_tile(w, 0);
         valid = t < (s ? w.tokens[1] : w.tokens[0]);
-        see_r = valid ? min(w.pos0 + from + t + 1, w.kv) : 0;   // this row sees positions [0, see_r)
+        see_r = valid ? min(w.pos0 + from + t + 1, w.kv) : INT_MAX;   // this row sees positions [0, see_r); one that
+                                                                         // does not exist need not be masked
         item = (static_cast<size_t>(w.row0) + from + t) * a.H + w.hk * a.G + g;
         split = w.split;
         __syncwarp();
@@ -562,13 +673,21 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         ld_wait(x[0]);
 #pragma unroll
         for (int c = 1; c < 4; ++c) ld_tie(x[c]);
+        if (Lay::kEarly) {                   // S is in registers: the next scores may come
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(s_free + 8 * s);
+        }
         const int vis = see_r - j * kTile;   // columns below vis are visible
-        if (vis < kTile) {
+        if (__any_sync(0xffffffffu, vis < kTile)) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 4; ++c) {
+            const int n = vis - c * 32;
+            const uint32_t seen = n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (c * 32 + i >= vis) x[c][i] = 0xFF800000u;   // -inf
+              if (!(seen & (1u << i))) x[c][i] = 0xFF800000u;   // -inf
+          }
         }
         float top[4];
 #pragma unroll
@@ -585,9 +704,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           m = mx;
           l *= f;
         }
-        __syncwarp();
+        if (Lay::kEarly && j > j0) {         // the last P has been read (and O has its product)
+          if (!wait_warp(o_full + 8 * s, n_o++ & 1)) { ok = false; break; }
+          tc_fence_after();
+        }
         if (j > j0 && __any_sync(0xffffffffu, f != 1.f)) {
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < HD / 32; ++c) {
             uint32_t o[32];
             ld32(to + c * 32, o);
@@ -612,7 +734,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
             sum[i & 1] = add2(sum[i & 1], pair(e0, e1));
             p[i] = pack_bf16(e0, e1);
           }
-          st16(ts + c * 16, p);
+          st16(tp + c * 16, p);
           if (c & 1) {                       // half of the tile's probabilities are there
             st_wait();
             tc_fence_before();
@@ -630,30 +752,41 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       const float inv = l > 0.f ? 1.f / l : 0.f;
       const size_t n_items = static_cast<size_t>(a.M) * a.H;
       const size_t part = (2 * static_cast<size_t>(split) + (solo ? s : 0)) * n_items + item;
+      // The results leave through a panel of 32 rows x 128 bytes, so that a store covers whole rows: straight from
+      // the lanes, each with a row of its own, every 16 bytes took a pass of the store path (7000 cycles a piece).
+      const unsigned rows_valid = __ballot_sync(0xffffffffu, valid);
+      const bool to_parts = a.n_splits > 1;
+      unsigned char* base = to_parts ? reinterpret_cast<unsigned char*>(a.part_o) : reinterpret_cast<unsigned char*>(a.out);
+      const size_t row_at = to_parts ? part * HD * 4 : item * HD * 2;
+      auto flush = [&](int byte0) {          // the panel to bytes byte0 .. byte0 + 127 of the rows
+        __syncwarp();
 #pragma unroll
-      for (int c = 0; c < HD / 32; ++c) {
+        for (int i = 0; i < 8; ++i) {
+          const int row = i * 4 + lane / 8, c = lane % 8;
+          const uint4 v = *reinterpret_cast<const uint4*>(panel + row * 128 + ((c ^ (row & 7)) * 16));
+          const size_t at = __shfl_sync(0xffffffffu, static_cast<unsigned long long>(row_at), row);
+          if (rows_valid >> row & 1) *reinterpret_cast<uint4*>(base + at + byte0 + c * 16) = v;
+        }
+        __syncwarp();
+      };
+#pragma unroll 1
+      for (int c = 0; c < HD / 32; ++c) {    // (not unrolled: the code of a rare path is fetched each time)
         uint32_t o[32];
         ld32(to + c * 32, o);
         ld_wait(o);
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = l > 0.f ? __float_as_uint(__uint_as_float(o[i]) * inv) : 0u;
-        if (valid) {
-          if (a.n_splits > 1) {
-            float* dst = a.part_o + part * HD + c * 32;
+        const int k0 = to_parts ? 0 : (c & 1) * 4;
+        if (!to_parts) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(dst + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
-          } else {
-            bf16* dst = a.out + item * HD + c * 32;
-#pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              uint32_t v[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                v[e] = pack_bf16(__uint_as_float(o[i + 2 * e]), __uint_as_float(o[i + 2 * e + 1]));
-              *reinterpret_cast<uint4*>(dst + i) = make_uint4(v[0], v[1], v[2], v[3]);
-            }
-          }
+          for (int i = 0; i < 16; ++i) o[i] = pack_bf16(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1]));
         }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < 4 || to_parts)
+            *reinterpret_cast<uint4*>(panel + lane * 128 + (((k0 + k) ^ (lane & 7)) * 16)) =
+                make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+        if (to_parts || (c & 1)) flush(to_parts ? c * 128 : (c >> 1) * 128);
       }
       if (valid) {
         const float l2 = l > 0.f ? m + log2f(l) : -INFINITY;
@@ -672,32 +805,60 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
   if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-// Joins the splits of each (row, head): o = sum_z w_z o_z / sum_z w_z, w_z = 2^{lse_z - max}. A warp each.
-template <int HD>
+// Joins the partial results of each (row, head): o = sum_z w_z o_z / sum_z w_z, w_z = 2^{lse_z - max}. W warps
+// per item, each taking every W-th partial result, eight loads in flight.
+template <int HD, int W>
 __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant__ PromptArgs a) {
+  constexpr int kPer = HD / 32, kAhead = 8;
+  struct alignas(4 * kPer) Vec { float v[kPer]; };
   pdl_wait();
-  const int lane = threadIdx.x & 31;
-  const size_t item = static_cast<size_t>(blockIdx.x) * 4 + (threadIdx.x >> 5), n = static_cast<size_t>(a.M) * a.H;
-  if (item >= n || static_cast<int>(item / a.H) >= a.cu[a.n_seq]) return;
+  __shared__ float acc_s[4][HD + 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % W;
+  const size_t item = static_cast<size_t>(blockIdx.x) * (4 / W) + warp / W, n = static_cast<size_t>(a.M) * a.H;
+  const int parts = item < n ? 2 * a.n_splits : 0;
+  const int rows = a.cu[a.n_seq];
   float mx = -INFINITY;
-  const int parts = 2 * a.n_splits;
   for (int z = lane; z < parts; z += 32) mx = fmaxf(mx, a.part_lse[z * n + item]);
   mx = warp_max(mx);
   const float base = mx == -INFINITY ? 0.f : mx;
-  constexpr int kPer = HD / 32;
   float acc[kPer] = {}, total = 0.f;
-  for (int z = 0; z < parts; ++z) {
-    const float w = ex2(a.part_lse[z * n + item] - base);
-    if (w == 0.f) continue;                // nothing seen there (or nothing written)
-    total += w;
-    const float* o = a.part_o + (z * n + item) * HD + lane * kPer;
+  for (int z0 = sub; z0 < parts; z0 += W * kAhead) {
+    float w[kAhead];
+    Vec o[kAhead];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] += w * o[i];
+    for (int i = 0; i < kAhead; ++i) w[i] = z0 + i * W < parts ? a.part_lse[(z0 + i * W) * n + item] : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      o[i] = Vec{};                        // (where nothing was seen nothing may have been written)
+      if (w[i] > -INFINITY) o[i] = *reinterpret_cast<const Vec*>(a.part_o + ((z0 + i * W) * n + item) * HD + lane * kPer);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      w[i] = ex2(w[i] - base);
+      total += w[i];
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[e] += w[i] * o[i].v[e];
+    }
   }
-  const float inv = total > 0.f ? 1.f / total : 0.f;
+  if (W > 1) {
 #pragma unroll
-  for (int i = 0; i < kPer; i += 2)
-    *reinterpret_cast<uint32_t*>(a.out + item * HD + lane * kPer + i) = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
+    for (int e = 0; e < kPer; ++e) acc_s[warp][lane * kPer + e] = acc[e];
+    if (lane == 0) acc_s[warp][HD] = total;
+    __syncthreads();
+    if (sub) return;
+#pragma unroll
+    for (int i = 1; i < W; ++i) {
+      total += acc_s[warp + i][HD];
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[e] += acc_s[warp + i][lane * kPer + e];
+    }
+  }
+  if (item >= n || static_cast<int>(item / a.H) >= rows) return;
+  const float inv = total > 0.f ? 1.f / total : 0.f;
+  struct alignas(2 * kPer) Out { uint32_t v[kPer / 2]; } out;
+#pragma unroll
+  for (int i = 0; i < kPer; i += 2) out.v[i / 2] = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
+  *reinterpret_cast<Out*>(a.out + item * HD + lane * kPer) = out;
   if (a.lse && lane == 0) a.lse[item] = total > 0.f ? (mx + log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
@@ -728,10 +889,11 @@ cudaError_t launch(const PromptArgs& a, int tiles, cudaStream_t st) {
   constexpr int smem = Layout<HD>::kSmem;
   cudaError_t e = cudaFuncSetAttribute(prompt_attention_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  prompt_attention_kernel<HD><<<dim3(tiles, a.Hkv, a.n_splits), kThreads, smem, st>>>(a);
+  prompt_attention_kernel<HD><<<dim3(a.Hkv, tiles, a.n_splits), kThreads, smem, st>>>(a);
   if ((e = cudaGetLastError()) != cudaSuccess || a.n_splits == 1) return e;
-  const unsigned grid = static_cast<unsigned>((static_cast<long long>(a.M) * a.H + 3) / 4);
-  return launch_pdl(prompt_join_kernel<HD>, dim3(grid), dim3(128), 0, st, a);
+  const long long items = static_cast<long long>(a.M) * a.H;
+  if (a.n_splits <= 4) return launch_pdl(prompt_join_kernel<HD, 1>, dim3(static_cast<unsigned>((items + 3) / 4)), dim3(128), 0, st, a);
+  return launch_pdl(prompt_join_kernel<HD, 4>, dim3(static_cast<unsigned>(items)), dim3(128), 0, st, a);
 }
 
 }  // namespace
@@ -777,8 +939,13 @@ sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t
   a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(d_workspace) + 256);
   a.part_lse = a.part_o + static_cast<size_t>(2 * s.splits) * M * H * hd;
   const bf16* pool = static_cast<const bf16*>(d_pool) + static_cast<size_t>(layer) * n_blocks * 2 * Hkv * kPage * hd;
-  if (!encode_weight_map(&a.map_kv, pool, a.kv_rows, hd, kPage) ||
-      !encode_rows_map(&a.map_q, d_q, hd, H, M, ldq, s.G, s.T))
+  a.pool = pool;
+  // Q: [row][head][hd], boxes of T rows x G heads x 64; K: [page row][hd], a page x 64; V: a page x all of hd,
+  // one 64-column half behind the other
+  const long long kv_rows = a.kv_rows;
+  if (!encode_map3(&a.map_q, d_q, {hd, H, M}, {hd, ldq}, {64, s.G, s.T}) ||
+      !encode_map3(&a.map_k, pool, {hd, kv_rows, 1}, {hd, kv_rows * hd}, {64, kPage, 1}) ||
+      !encode_map3(&a.map_v, pool, {64, kv_rows, hd / 64}, {hd, 64}, {64, kPage, hd / 64}))
     return fail(SD2_ECUDA, "prompt attention: tensor map");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = hd == 64 ? launch<64>(a, s.tiles, st) : launch<128>(a, s.tiles, st);
