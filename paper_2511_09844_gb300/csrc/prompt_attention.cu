@@ -62,7 +62,7 @@ struct Layout {
   static constexpr int kSlotBytes = kTile * HD * 2;     // a query tile, or a K or V tile
   static constexpr int kHalf = kTile * 128;             // its 64-column half (of Q and K; V lies page by page)
   static constexpr int kPageBytes = kPage * HD * 2;
-  static constexpr int kStages = HD == 128 ? 4 : 8;
+  static constexpr int kStages = HD == 128 ? 4 : 8;     // (a power of two)
   static constexpr int kStaging = 8 * 4096;             // a 4 KB panel per softmax warp for the results' way out
   static constexpr int kBytes = (2 + kStages) * kSlotBytes + kStaging;
   // TMEM columns: S of each slot, then O, then P: over S where TMEM is full (hd 128)
@@ -89,21 +89,28 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
       "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
       : "memory");
 }
-// D += A B with A (bf16 pairs, one row per lane) in TMEM.
-__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                            uint32_t accumulate) {
+// Shared-memory descriptors (128-byte swizzle), their low words (address and leading byte offset; the high
+// word is a constant: groups of 8 rows 1024 bytes apart, version 1). K-major: rows of 128 bytes. MN-major:
+// each k is a row of 64 contiguous MN elements, the next 64 `mn_stride` bytes on (leading byte offset).
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_k(uint32_t saddr) { return (saddr >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_mn(uint32_t saddr, uint32_t mn_stride) {
+  return (saddr >> 4) | ((mn_stride >> 4) << 16);
+}
+// D (+)= A B, both operands in shared memory, or A (bf16 pairs, one row per lane) in TMEM.
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_desc, uint32_t b_desc, uint32_t idesc, uint32_t add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(
-          d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d_tmem),
+      "r"(a_desc), "r"(b_desc), "r"(idesc), "r"(add), "n"(kDescHigh)
       : "memory");
 }
-// Descriptor of an MN-major tile with the 128-byte swizzle: each k is a row of 64 contiguous MN elements
-// (128 bytes), 8 rows per 1024-byte group (stride byte offset between groups along k), the next 64 MN
-// elements `mn_stride` bytes on (leading byte offset).
-__device__ __forceinline__ uint64_t sw128_mn_desc(uint32_t saddr, uint32_t mn_stride) {
-  return (sw128_desc(saddr) & ~(static_cast<uint64_t>(0x3FFF) << 16)) |
-         (static_cast<uint64_t>((mn_stride & 0x3FFFFu) >> 4) << 16);
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_desc, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 b;\n mov.b64 b, {%2, %5};\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_desc), "r"(idesc), "r"(add), "n"(kDescHigh)
+      : "memory");
 }
 
 #define SD2_R16(v, o) "=r"(v[o]), "=r"(v[o + 1]), "=r"(v[o + 2]), "=r"(v[o + 3]), "=r"(v[o + 4]), "=r"(v[o + 5]), \
@@ -172,24 +179,29 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&t);
 }
 
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 // Bounded wait of the MMA thread: polls (a suspended wait wakes up some hundred cycles late).
 __device__ __forceinline__ bool wait_spin(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned* err) {
-  const long long t0 = clock64();
+  if (mbar_test(bar, parity)) return true;
+  long long t0 = 0;
   for (uint32_t it = 1;; ++it) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    if (ok) return true;
-    if ((it & 63) == 0) {
-      if (*abort_flag) return false;
-      if (clock64() - t0 > kWaitCycles) {
-        *abort_flag = 1;
-        atomicOr(err, static_cast<unsigned>(ERR_TIMEOUT));
-        return false;
-      }
+    if (mbar_test(bar, parity)) return true;
+    if (it & 255) continue;
+    if (*abort_flag) return false;
+    const long long t = clock64();
+    if (!t0) t0 = t;
+    if (t - t0 > kWaitCycles) {
+      *abort_flag = 1;
+      atomicOr(err, static_cast<unsigned>(ERR_TIMEOUT));
+      return false;
     }
   }
 }
@@ -482,50 +494,65 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           if (i < u) wait_bar_budget(full0 + 8 * i, ((u - 1 - i) / S) & 1, kDrainCycles);
       }
     } else if (warp == 9) {
+      // The products. This thread's own instructions are the limit between the waits (a turn of one slot is 1024
+      // cycles of products for hd 128, 512 for hd 64, in some 16 or 12 instructions of 10 to 40 cycles), so whole
+      // tiles of both slots run in a loop without a condition; what is left of a piece goes tile by tile.
       if (elect_one()) {
         auto wait = [&](uint32_t bar, uint32_t parity) { return wait_spin(bar, parity, abort_flag, a.err); };
+        constexpr uint32_t kSlot16 = Lay::kSlotBytes >> 4, kHalf16 = Lay::kHalf >> 4, kPage16 = Lay::kPageBytes >> 4;
         const uint32_t idesc_s = idesc_bf16(kTile, 0), idesc_o = idesc_bf16(kTile, HD) | (1u << 16);   // B of P V is MN-major
-        const uint64_t q_desc = sw128_desc(q_smem);
+        const uint32_t q_desc = desc_k(q_smem), k_desc = desc_k(kv_smem), v_desc = desc_mn(kv_smem, kPage * 128);
         Work w;
         bool ok = true;
-        uint32_t st = 0, ph = 0, n_q = 0;                      // ring position of the next tile, Q tiles so far
+        uint32_t u = 0, n_q = 0;                               // tiles taken from the ring, Q tiles so far
         uint32_t n_p[2] = {0, 0}, n_sc[2] = {0, 0};            // P and S tiles so far
-        auto advance = [&]() { if (++st == S) { st = 0; ph ^= 1u; } };
+        auto stage = [&](uint32_t i) { return i & (S - 1); };
+        auto full = [&](uint32_t i) { return wait(full0 + 8 * stage(i), (i / S) & 1); };
+        auto issue_s = [&](int s, uint32_t a_desc, uint32_t st, uint32_t id) {
+          const uint32_t b_desc = k_desc + st * kSlot16;
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint32_t off = (kk / 4) * kHalf16 + (kk % 4) * 2;
+            mma_ss(tmem + s * kTile, a_desc + off, b_desc + off, id, kk > 0);
+          }
+        };
+        auto issue_o = [&](int s, uint32_t st, int part, uint32_t add) {
+          const uint32_t p = tmem + Lay::kP + s * Lay::kPStride, b_desc = v_desc + st * kSlot16;
+#pragma unroll
+          for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
+            mma_ts(tmem + Lay::kO + s * HD, p + kk * 8, b_desc + kk * kPage16, idesc_o, kk > 0 ? 1u : add);
+        };
         while (ok && next_work(w, wait)) {
           done_reading();
           if (w.jb >= w.je) continue;
           const int step = 1 + w.solo;
           const int last[2] = {last_tile(w, 0), last_tile(w, 1)};
           auto active = [&](int s, int j) { return j < last[s] && (!w.solo || ((j - w.jb) & 1) == s); };
-          auto scores = [&](int s, int j, uint32_t k_st) {     // S_s = Q_s K_j^T over the pages that the slot sees
+          auto scores = [&](int s, int j, uint32_t st) {       // S_s = Q_s K_j^T over the pages that the slot sees
             if (Lay::kEarly) {                                 // the softmax has taken the last scores
               if (!wait(s_free + 8 * s, (n_sc[s] & 1) ^ 1)) { ok = false; return; }
               tc_fence_after();
             }
             ++n_sc[s];
             const int n = min(kTile, ((s ? w.end[1] : w.end[0]) - j * kTile + kPage - 1) / kPage * kPage);
-            const uint32_t id = idesc_s | (static_cast<uint32_t>(n >> 3) << 17);
-            const uint64_t ad = q_desc + (w.solo ? 0 : (s * Lay::kSlotBytes) >> 4), bd = sw128_desc(kv_smem + k_st * Lay::kSlotBytes);
-#pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk) {
-              const uint64_t off = (kk / 4) * (Lay::kHalf >> 4) + (kk % 4) * 2;
-              mma_bf16(tmem + s * kTile, ad + off, bd + off, id, kk > 0);
-            }
+            issue_s(s, q_desc + (w.solo ? 0 : s * kSlot16), st, idesc_s | (static_cast<uint32_t>(n >> 3) << 17));
             mma_commit(s_full + 8 * s);
           };
-          auto values = [&](int s, int j, uint32_t v_smem) {   // O_s += P_s V_j, the halves of P as they come
+          auto values = [&](int s, int j, uint32_t st) {       // O_s += P_s V_j, the halves of P as they come
             const int steps = min(kTile / kPage, ((s ? w.end[1] : w.end[0]) - j * kTile + kPage - 1) / kPage);
-            const uint64_t bd = sw128_mn_desc(v_smem, kPage * 128);
-            const uint32_t more = j >= w.jb + step ? 1u : 0u;
+            const uint32_t add = j >= w.jb + step ? 1u : 0u;
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
               if (!ok || !wait(p_full + 16 * s + 8 * part, n_p[s] & 1)) { ok = false; continue; }
               tc_fence_after();
-#pragma unroll
-              for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
-                if (kk < steps)
-                  mma_bf16_ts(tmem + Lay::kO + s * HD, tmem + Lay::kP + s * Lay::kPStride + kk * 8,
-                              bd + kk * (Lay::kPageBytes >> 4), idesc_o, kk > 0 ? 1u : more);
+              if (steps == kTile / kPage) {
+                issue_o(s, st, part, add);
+              } else {
+#pragma unroll 1
+                for (int kk = 4 * part; kk < min(steps, 4 * part + 4); ++kk)
+                  mma_ts(tmem + Lay::kO + s * HD, tmem + Lay::kP + s * Lay::kPStride + kk * 8,
+                         v_desc + st * kSlot16 + kk * kPage16, idesc_o, kk > 0 ? 1u : add);
+              }
             }
             ++n_p[s];
             // O has tile j (where the next scores follow P in its columns, their barrier says so too)
@@ -534,23 +561,88 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           if (!(ok = wait(q_full, n_q & 1))) break;
           ++n_q;
           const int head = min(step, w.je - w.jb);             // K tiles before the first V tile
-          for (int i = 0; i < head && ok; ++i) {
-            if (!(ok = wait(full0 + 8 * st, ph))) break;
+          for (int i = 0; i < head && ok; ++i, ++u) {
+            if (!(ok = full(u))) break;
             tc_fence_after();
 #pragma unroll
             for (int s = 0; s < 2; ++s)
-              if (ok && active(s, w.jb + i)) scores(s, w.jb + i, st);
-            mma_commit(empty0 + 8 * st);
-            advance();
+              if (ok && active(s, w.jb + i)) scores(s, w.jb + i, stage(u));
+            mma_commit(empty0 + 8 * stage(u));
           }
           if (ok && w.jb + head == w.je) mma_commit(q_empty);  // every product that reads Q has been issued
+          // tiles j whose successor is whole for both slots
+          const int whole = w.solo ? 0 : min(w.je - 1, min(w.end[0], w.end[1]) / kTile - 1);
           for (int j = w.jb; j < w.je && ok; ++j) {
+            if (j > w.jb && j < whole) {
+              constexpr uint32_t id = (1u << 4) | (1u << 7) | (1u << 10) | ((kTile >> 3) << 17) | ((kTile >> 4) << 24);
+              uint32_t p0 = n_p[0] & 1, p1 = n_p[1] & 1, c0 = n_sc[0] & 1, c1 = n_sc[1] & 1;
+              const int n = whole - j;
+              int i = 0;
+              for (; i < n; ++i, u += 2) {
+                const uint32_t st0 = stage(u), st1 = stage(u + 1);
+                if (Lay::kEarly) {
+                  if (!full(u) || !wait(s_free, c0 ^ 1)) break;
+                  tc_fence_after();
+                  issue_s(0, q_desc, st0, id);
+                  mma_commit(s_full);
+                  if (!wait(s_free + 8, c1 ^ 1)) break;
+                  tc_fence_after();
+                  issue_s(1, q_desc + kSlot16, st0, id);
+                  mma_commit(s_full + 8);
+                  mma_commit(empty0 + 8 * st0);
+                  if (!full(u + 1)) break;
+                  if (!wait(p_full, p0)) break;
+                  tc_fence_after();
+                  issue_o(0, st1, 0, 1);
+                  if (!wait(p_full + 8, p0)) break;
+                  tc_fence_after();
+                  issue_o(0, st1, 1, 1);
+                  mma_commit(o_full);
+                  if (!wait(p_full + 16, p1)) break;
+                  tc_fence_after();
+                  issue_o(1, st1, 0, 1);
+                  if (!wait(p_full + 24, p1)) break;
+                  tc_fence_after();
+                  issue_o(1, st1, 1, 1);
+                  mma_commit(o_full + 8);
+                  mma_commit(empty0 + 8 * st1);
+                } else {
+                  if (!full(u) || !wait(p_full, p0)) break;
+                  tc_fence_after();
+                  issue_o(0, st0, 0, 1);
+                  if (!wait(p_full + 8, p0)) break;
+                  tc_fence_after();
+                  issue_o(0, st0, 1, 1);
+                  if (!full(u + 1)) break;
+                  tc_fence_after();
+                  issue_s(0, q_desc, st1, id);
+                  mma_commit(s_full);
+                  if (!wait(p_full + 16, p1)) break;
+                  tc_fence_after();
+                  issue_o(1, st0, 0, 1);
+                  if (!wait(p_full + 24, p1)) break;
+                  tc_fence_after();
+                  issue_o(1, st0, 1, 1);
+                  mma_commit(empty0 + 8 * st0);
+                  issue_s(1, q_desc + kSlot16, st1, id);
+                  mma_commit(s_full + 8);
+                  mma_commit(empty0 + 8 * st1);
+                }
+                p0 ^= 1; p1 ^= 1; c0 ^= 1; c1 ^= 1;
+              }
+              if (i < n) { ok = false; break; }
+#pragma unroll
+              for (int s = 0; s < 2; ++s) { n_p[s] += n; n_sc[s] += n; }
+              if (whole == w.je - 1) mma_commit(q_empty);
+              j = whole - 1;
+              continue;
+            }
             const bool k_next = j + step < w.je;
             uint32_t k_st = 0, v_st = 0;
             auto take = [&](uint32_t& x) {                     // the next tile of the ring
-              x = st;
-              if (!wait(full0 + 8 * st, ph)) { ok = false; return; }
-              advance();
+              x = stage(u);
+              if (!full(u)) { ok = false; return; }
+              ++u;
               tc_fence_after();
             };
             if (Lay::kEarly) {
@@ -564,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
               if (ok) take(v_st);
 #pragma unroll
               for (int s = 0; s < 2; ++s)
-                if (ok && active(s, j)) values(s, j, kv_smem + v_st * Lay::kSlotBytes);
+                if (ok && active(s, j)) values(s, j, v_st);
               if (ok) mma_commit(empty0 + 8 * v_st);
             } else {
               bool have_k = false;
@@ -572,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
 #pragma unroll
               for (int s = 0; s < 2; ++s) {
                 if (!ok || !active(s, j)) continue;
-                values(s, j, kv_smem + v_st * Lay::kSlotBytes);
+                values(s, j, v_st);
                 if (!ok || j + step >= last[s]) continue;
                 if (!have_k) take(k_st);
                 have_k = true;
