@@ -781,62 +781,80 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
               if (!(seen & (1u << i))) x[c][i] = 0xFF800000u;   // -inf
           }
         }
-        float top[4];
+        auto tile_max = [&]() {
+          float top[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          top[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
+          for (int c = 0; c < 4; ++c) {
+            top[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
 #pragma unroll
-          for (int i = 2; i < 32; i += 2) top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])));
-        }
-        float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-        mx *= scale;
-        float f = 1.f;
-        if (mx > m + kGrowth || (m == -INFINITY && mx > m)) {
-          f = ex2(m - mx);
-          m = mx;
-          l *= f;
-        }
+            for (int i = 2; i < 32; i += 2)
+              top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])));
+          }
+          return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
+        };
+        // probabilities of columns 64 h .. 64 h + 63 as packed bf16, and their sum (of the unrounded ones)
+        auto half_exp = [&](int h, uint32_t (&p)[2][16]) {
+          const float base = m == -INFINITY ? 0.f : m;
+          const uint64_t scale2 = pair(scale, scale), base2 = pair(-base, -base);
+          uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const uint32_t* v = x[2 * h + c] + 2 * i;
+              float e0, e1;
+              unpair(fma2(pair(__uint_as_float(v[0]), __uint_as_float(v[1])), scale2, base2), e0, e1);
+              e0 = ex2(e0);
+              e1 = ex2(e1);
+              sum[i & 1] = add2(sum[i & 1], pair(e0, e1));
+              p[c][i] = pack_bf16(e0, e1);
+            }
+          float s0, s1;
+          unpair(add2(sum[0], sum[1]), s0, s1);
+          return s0 + s1;
+        };
+        // The first half is computed under the last maximum while this tile's is found (the two need different
+        // units); only if that has grown too much, or there is none yet, it is computed again.
+        uint32_t p[2][16];
+        const float mx = tile_max();
+        float part = half_exp(0, p);
+        const bool grown = mx > m + kGrowth || (m == -INFINITY && mx > m);
         if (Lay::kEarly && j > j0) {         // the last P has been read (and O has its product)
           if (!wait_warp(o_full + 8 * s, n_o++ & 1)) { ok = false; break; }
           tc_fence_after();
         }
-        if (j > j0 && __any_sync(0xffffffffu, f != 1.f)) {
+        if (__any_sync(0xffffffffu, grown)) {
+          float f = 1.f;
+          if (grown) {
+            f = ex2(m - mx);
+            m = mx;
+            l *= f;
+          }
+          __syncwarp();
+          if (j > j0) {
 #pragma unroll 1
-          for (int c = 0; c < HD / 32; ++c) {
-            uint32_t o[32];
-            ld32(to + c * 32, o);
-            ld_wait(o);
+            for (int c = 0; c < HD / 32; ++c) {
+              uint32_t o[32];
+              ld32(to + c * 32, o);
+              ld_wait(o);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            st32(to + c * 32, o);
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              st32(to + c * 32, o);
+            }
           }
+          part = half_exp(0, p);
         }
-        const float base = m == -INFINITY ? 0.f : m;
-        const uint64_t scale2 = pair(scale, scale), base2 = pair(-base, -base);
-        uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t p[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float e0, e1;
-            unpair(fma2(pair(__uint_as_float(x[c][2 * i]), __uint_as_float(x[c][2 * i + 1])), scale2, base2), e0, e1);
-            e0 = ex2(e0);
-            e1 = ex2(e1);
-            sum[i & 1] = add2(sum[i & 1], pair(e0, e1));
-            p[i] = pack_bf16(e0, e1);
-          }
-          st16(tp + c * 16, p);
-          if (c & 1) {                       // half of the tile's probabilities are there
-            st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * (c >> 1));
-          }
+        for (int h = 0; h < 2; ++h) {
+          if (h) part += half_exp(1, p);
+          st16(tp + h * 32, p[0]);
+          st16(tp + h * 32 + 16, p[1]);
+          st_wait();                         // half of the tile's probabilities are there
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * h);
         }
-        float s0, s1;
-        unpair(add2(sum[0], sum[1]), s0, s1);
-        l += s0 + s1;
+        l += part;
       }
       if (je_s > j0 && ok) ok = wait_warp(o_full + 8 * s, n_o++ & 1);
       if (!ok) break;
@@ -961,17 +979,22 @@ sd2_status fail(sd2_status s, const std::string& m) {
 bool unaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
 // The grid: query tiles (an upper bound: the sequences' lengths are on the device), and splits of the
-// positions where tiles x KV heads leave SMs idle; a split keeps at least two K/V tiles.
+// positions where tiles x KV heads leave SMs idle. A split keeps at least two K/V tiles (one row on 1000
+// positions: 12.7 us with two, 14.9 with four, 19.1 with eight), and as many that the partial results, f32,
+// written and read once more, are no more than the K/V bytes it reads (512 rows on no cache, 8B heads: 25 us in
+// two splits, 13.7 in one).
 struct Shape {
   int G, T, tiles, splits;
 };
-Shape shape_of(int M, int n_seq, int H, int Hkv, int max_kv) {
+Shape shape_of(int M, int n_seq, int H, int Hkv, int hd, int max_kv) {
   Shape s;
   s.G = H / Hkv;
   s.T = kTile / s.G;
   s.tiles = static_cast<int>(std::min<long long>(M, M / (2 * s.T) + static_cast<long long>(n_seq)));
   const long long ctas = static_cast<long long>(s.tiles) * Hkv;
-  const long long most = (max_kv + 2 * kTile - 1) / (2 * kTile);
+  const long long rows = std::min<long long>(2 * kTile, static_cast<long long>(M) * s.G);   // query vectors of a tile
+  const long long keep = std::max<long long>(2 * kTile, 2 * rows);                           // positions of a split
+  const long long most = (max_kv + keep - 1) / keep;
   s.splits = static_cast<int>(std::max(1ll, std::min({most, sm_count_cached() / ctas, 128ll})));
   return s;
 }
@@ -997,7 +1020,7 @@ using namespace sd2;
 
 size_t sd2_attention_prompt_workspace_bytes(int32_t M, int32_t n_seq, int32_t H, int32_t Hkv, int32_t hd, int32_t max_kv) {
   if (M < 1 || n_seq < 1 || Hkv < 1 || H < Hkv || H % Hkv || (hd != 64 && hd != 128) || max_kv < 1) return 0;
-  const Shape s = shape_of(M, n_seq, H, Hkv, max_kv);
+  const Shape s = shape_of(M, n_seq, H, Hkv, hd, max_kv);
   const size_t parts = s.splits > 1 ? static_cast<size_t>(2 * s.splits) * M * H * (hd + 1) * 4 : 0;
   return 256 + (parts + 255) / 256 * 256;
 }
@@ -1021,7 +1044,7 @@ sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t
     return fail(SD2_EINVAL, "workspace too small");
   if (unaligned(d_workspace, 256)) return fail(SD2_EINVAL, "workspace not 256-byte aligned");
   if (M == 0) return SD2_OK;
-  const Shape s = shape_of(M, n_seq, H, Hkv, max_kv);
+  const Shape s = shape_of(M, n_seq, H, Hkv, hd, max_kv);
   PromptArgs a{};
   a.M = M; a.H = H; a.Hkv = Hkv; a.G = s.G; a.T = s.T; a.n_blocks = n_blocks; a.bt_stride = bt_stride;
   a.n_seq = n_seq; a.n_splits = s.splits; a.kv_rows = n_blocks * 2 * Hkv * kPage;
