@@ -443,48 +443,70 @@ def gemm(x: torch.Tensor, w: torch.Tensor, epilogue: int = 0, out: Optional[torc
     return h if epilogue in (2, 4) else out
 
 
-def _require(ok: bool, what: str):
+def _refuse(what: str):
     """Refuse what the C ABI cannot see: a tensor's device, type, shape or strides."""
-    if not ok:
-        raise SD2Error(SD2_EINVAL, what)
+    raise SD2Error(SD2_EINVAL, what)
 
 
 def _pool_shape(pool: torch.Tensor):
-    _require(pool.is_cuda and pool.dtype == torch.bfloat16 and pool.dim() == 6 and pool.is_contiguous() and
-             pool.shape[2] == 2 and pool.shape[4] == 16,
-             "pool must be a contiguous CUDA bf16 tensor [L, n_blocks, 2, Hkv, 16, hd]")
-    return pool.shape[0], pool.shape[1], pool.shape[3], pool.shape[5]
+    """(L, n_blocks, Hkv, hd, device index) of a paged cache."""
+    shape = pool.shape
+    if not (pool.is_cuda and pool.dtype == torch.bfloat16 and len(shape) == 6 and pool.is_contiguous() and
+            shape[2] == 2 and shape[4] == 16):
+        _refuse("pool must be a contiguous CUDA bf16 tensor [L, n_blocks, 2, Hkv, 16, hd]")
+    return shape[0], shape[1], shape[3], shape[5], pool.get_device()
 
 
-def _ints(name: str, t: Optional[torch.Tensor], *shape, device):
-    """An optional contiguous int32 tensor on the pool's device, of this shape."""
-    _require(t is None or (t.dtype == torch.int32 and t.device == device and t.is_contiguous() and
-                           tuple(t.shape) == shape),
-             f"{name} must be a contiguous int32 tensor {list(shape)} on the pool's device")
+def _ints(name: str, t: Optional[torch.Tensor], shape: tuple, index: int):
+    """The address of an optional contiguous int32 tensor of this shape on the pool's device."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous int32 tensor {list(shape)} on the pool's device")
+    return t.data_ptr()
 
 
-def _batch(table: torch.Tensor, cu_rows: torch.Tensor, kv_len: torch.Tensor, device):
-    _require(table.dim() == 2, "table must be int32 [n_seq, bt_stride]")
-    n, stride = table.shape
-    _ints("table", table, n, stride, device=device)
-    _ints("cu_rows", cu_rows, n + 1, device=device)
-    _ints("kv_len", kv_len, n, device=device)
-    return n, stride
+def _table_shape(table: torch.Tensor):
+    if table.dim() != 2:
+        _refuse("table must be int32 [n_seq, bt_stride]")
+    return table.shape
 
 
-def _rows(name: str, t: torch.Tensor, dtypes, hd: int, device):
-    """Packed rows [M, heads, hd] whose heads are back to back; any row stride. Returns the stride."""
-    _require(t.dim() == 3 and t.dtype in dtypes and t.device == device and t.shape[2] == hd and t.shape[1] >= 1 and
-             (t.numel() == 0 or (t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == hd))),
-             f"{name} must be rows [M, heads, {hd}] on the pool's device, each row's heads back to back")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * hd
+def _rows(name: str, t: torch.Tensor, dtypes, hd: int, index: int) -> int:
+    """Row stride of packed rows [M, heads, hd] whose heads are back to back."""
+    if t.dim() != 3 or t.dtype not in dtypes or t.get_device() != index:
+        _refuse(f"{name} must be rows [M, heads, {hd}] on the pool's device, of type {' or '.join(map(str, dtypes))}")
+    m, heads, width = t.shape
+    row, head, one = t.stride()
+    if width != hd or heads < 1 or (m and (one != 1 or (heads > 1 and head != hd))):
+        _refuse(f"{name} must be rows [M, heads, {hd}], each row's heads back to back")
+    return row if m > 1 else heads * hd
 
 
 def _workspace(given: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
     if given is None:
         return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
-    _require(given.device == device and given.is_contiguous(), "workspace must be contiguous, on the pool's device")
+    if given.device != device or not given.is_contiguous():
+        _refuse("workspace must be contiguous, on the pool's device")
     return given
+
+
+def _error_word(err: Optional[torch.Tensor], index: int):
+    if err is None:
+        return None
+    if err.dtype != torch.int32 or err.get_device() != index or err.numel() < 1:
+        _refuse("err must be an int32 tensor on the pool's device")
+    return err.data_ptr()
+
+
+# the current stream's handle without building a Stream object (2 us on the launching core), where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_handle(stream, index: int) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 def _used_on(stream, *tensors):
@@ -505,20 +527,24 @@ def attention_prompt(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, l
     bound of it (default: the table's room). Returns bf16 [M, H * hd], with f32 [M, H] log-sum-exps if
     `return_lse`. Rows of no sequence are left unwritten."""
     lib = load_library()
-    L, n_blocks, Hkv, hd = _pool_shape(pool)
-    dev = pool.device
-    n_seq, stride = _batch(table, cu_rows, kv_len, dev)
-    ldq = _rows("q", q, (torch.bfloat16,), hd, dev)
-    _require(0 <= layer < L, "layer outside the pool")
+    L, n_blocks, Hkv, hd, index = _pool_shape(pool)
+    device = pool.device
+    n_seq, stride = _table_shape(table)
+    ldq = _rows("q", q, (torch.bfloat16,), hd, index)
+    if not 0 <= layer < L:
+        _refuse("layer outside the pool")
     M, H, _ = q.shape
     max_kv = 16 * stride if max_kv is None else max(1, int(max_kv))
-    out = torch.empty((M, H * hd), dtype=torch.bfloat16, device=dev)
-    lse = torch.empty((M, H), dtype=torch.float32, device=dev) if return_lse else None
+    batch = (_ints("table", table, (n_seq, stride), index), _ints("cu_rows", cu_rows, (n_seq + 1,), index),
+             _ints("kv_len", kv_len, (n_seq,), index))
+    out = torch.empty((M, H * hd), dtype=torch.bfloat16, device=device)
+    lse = torch.empty((M, H), dtype=torch.float32, device=device) if return_lse else None
     if M:
-        ws = _workspace(workspace, lib.sd2_attention_prompt_workspace_bytes(M, n_seq, H, Hkv, hd, max_kv), dev)
-        _check(lib, lib.sd2_attention_prompt(_ptr(q), ldq, M, H, Hkv, hd, _ptr(pool), n_blocks, _ptr(table), stride, layer,
-                                             _ptr(cu_rows), _ptr(kv_len), n_seq, max_kv, _ptr(out), _ptr(lse), _ptr(ws),
-                                             ws.numel() * ws.element_size(), _ptr(err), _stream(stream)))
+        ws = _workspace(workspace, lib.sd2_attention_prompt_workspace_bytes(M, n_seq, H, Hkv, hd, max_kv), device)
+        _check(lib, lib.sd2_attention_prompt(q.data_ptr(), ldq, M, H, Hkv, hd, pool.data_ptr(), n_blocks, batch[0], stride,
+                                             layer, batch[1], batch[2], n_seq, max_kv, out.data_ptr(),
+                                             None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
+                                             _error_word(err, index), _stream_handle(stream, index)))
         _used_on(stream, out, lse, ws)
     return (out, lse) if return_lse else out
 
@@ -529,18 +555,21 @@ def pages_append(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor, table: to
     bf16, any row stride (views of a fused projection's output will do); the batch as in
     attention_prompt."""
     lib = load_library()
-    L, n_blocks, Hkv, hd = _pool_shape(pool)
-    dev = pool.device
-    n_seq, stride = _batch(table, cu_rows, kv_len, dev)
-    _require(0 <= layer < L, "layer outside the pool")
-    _require(k.shape == v.shape and k.dtype == v.dtype and k.dim() == 3 and k.shape[1] == Hkv,
-             "k and v must have one type and the shape [M, Hkv, hd]")
-    ldk = _rows("k", k, (torch.float32, torch.bfloat16), hd, dev)
-    ldv = _rows("v", v, (torch.float32, torch.bfloat16), hd, dev)
+    L, n_blocks, Hkv, hd, index = _pool_shape(pool)
+    n_seq, stride = _table_shape(table)
+    if not 0 <= layer < L:
+        _refuse("layer outside the pool")
+    if k.shape != v.shape or k.dtype != v.dtype or k.dim() != 3 or k.shape[1] != Hkv:
+        _refuse("k and v must have one type and the shape [M, Hkv, hd]")
+    ldk = _rows("k", k, (torch.float32, torch.bfloat16), hd, index)
+    ldv = _rows("v", v, (torch.float32, torch.bfloat16), hd, index)
+    batch = (_ints("table", table, (n_seq, stride), index), _ints("cu_rows", cu_rows, (n_seq + 1,), index),
+             _ints("kv_len", kv_len, (n_seq,), index))
     if k.shape[0]:
-        _check(lib, lib.sd2_pages_append(_ptr(k), ldk, _ptr(v), ldv, DTYPE_BF16 if k.dtype == torch.bfloat16 else DTYPE_F32,
-                                         k.shape[0], Hkv, hd, _ptr(pool), n_blocks, _ptr(table), stride, layer,
-                                         _ptr(cu_rows), _ptr(kv_len), n_seq, _ptr(err), _stream(stream)))
+        _check(lib, lib.sd2_pages_append(k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                         DTYPE_BF16 if k.dtype == torch.bfloat16 else DTYPE_F32, k.shape[0], Hkv, hd,
+                                         pool.data_ptr(), n_blocks, batch[0], stride, layer, batch[1], batch[2], n_seq,
+                                         _error_word(err, index), _stream_handle(stream, index)))
 
 
 class ForkedPages(NamedTuple):
@@ -558,21 +587,23 @@ def pages_fork(pool: torch.Tensor, table: torch.Tensor, length: torch.Tensor, pa
     none) after its first keep[b] positions, with room for grow[b] more. Sequences that no parent entry
     names give up their pages; whole pages are shared, shared tails copied."""
     lib = load_library()
-    L, n_blocks, Hkv, hd = _pool_shape(pool)
-    dev = pool.device
-    _require(table.dim() == 2 and parent.dim() == 1 and parent.numel() > 0, "table must be 2-D and parent 1-D, not empty")
-    (n_seq, stride), n = table.shape, parent.numel()
-    _ints("table", table, n_seq, stride, device=dev)
-    _ints("length", length, n_seq, device=dev)
-    for name, t in (("parent", parent), ("keep", keep), ("grow", grow)):
-        _ints(name, t, n, device=dev)
-    _ints("pinned", pinned, n_blocks, device=dev)
-    f = ForkedPages(torch.empty((n, stride), dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev),
-                    torch.empty(n, dtype=torch.int32, device=dev), torch.empty(n_blocks, dtype=torch.int32, device=dev))
-    ws = _workspace(workspace, lib.sd2_pages_fork_workspace_bytes(n, n_blocks), dev)
-    _check(lib, lib.sd2_pages_fork(_ptr(pool), L, n_blocks, Hkv, hd, _ptr(table), stride, _ptr(length), n_seq, _ptr(parent),
-                                   _ptr(keep), _ptr(grow), _ptr(pinned), n, _ptr(f.table), _ptr(f.length), _ptr(f.pages),
-                                   _ptr(f.ref), _ptr(ws), ws.numel() * ws.element_size(), _ptr(err), _stream(stream)))
+    L, n_blocks, Hkv, hd, index = _pool_shape(pool)
+    device = pool.device
+    n_seq, stride = _table_shape(table)
+    if parent.dim() != 1 or parent.numel() < 1:
+        _refuse("parent must be 1-D, not empty")
+    n = parent.numel()
+    ins = (_ints("table", table, (n_seq, stride), index), _ints("length", length, (n_seq,), index),
+           _ints("parent", parent, (n,), index), _ints("keep", keep, (n,), index), _ints("grow", grow, (n,), index),
+           _ints("pinned", pinned, (n_blocks,), index))
+    f = ForkedPages(torch.empty((n, stride), dtype=torch.int32, device=device),
+                    torch.empty(n, dtype=torch.int32, device=device), torch.empty(n, dtype=torch.int32, device=device),
+                    torch.empty(n_blocks, dtype=torch.int32, device=device))
+    ws = _workspace(workspace, lib.sd2_pages_fork_workspace_bytes(n, n_blocks), device)
+    _check(lib, lib.sd2_pages_fork(pool.data_ptr(), L, n_blocks, Hkv, hd, ins[0], stride, ins[1], n_seq, ins[2], ins[3],
+                                   ins[4], ins[5], n, f.table.data_ptr(), f.length.data_ptr(), f.pages.data_ptr(),
+                                   f.ref.data_ptr(), ws.data_ptr(), ws.nbytes, _error_word(err, index),
+                                   _stream_handle(stream, index)))
     _used_on(stream, *f, ws)
     return f
 
@@ -590,18 +621,18 @@ def pages_compact(pool: torch.Tensor, table: torch.Tensor, pages: torch.Tensor, 
     """Move the pool's live pages (ref > 0) to the lowest ids (sd2_pages_compact); `pages` [n_seq] are the
     entries in use of each table row."""
     lib = load_library()
-    L, n_blocks, Hkv, hd = _pool_shape(pool)
-    dev = pool.device
-    _require(table.dim() == 2, "table must be int32 [n_seq, bt_stride]")
-    n_seq, stride = table.shape
-    _ints("table", table, n_seq, stride, device=dev)
-    _ints("pages", pages, n_seq, device=dev)
-    _ints("ref", ref, n_blocks, device=dev)
-    c = CompactedPages(torch.empty_like(table), torch.empty_like(ref), torch.empty_like(ref),
-                       torch.empty(1, dtype=torch.int32, device=dev))
-    ws = _workspace(workspace, lib.sd2_pages_compact_workspace_bytes(n_blocks), dev)
-    _check(lib, lib.sd2_pages_compact(_ptr(pool), L, n_blocks, Hkv, hd, _ptr(table), stride, _ptr(pages), n_seq, _ptr(ref),
-                                      _ptr(c.table), _ptr(c.ref), _ptr(c.map), _ptr(c.n_live), _ptr(ws),
-                                      ws.numel() * ws.element_size(), _ptr(err), _stream(stream)))
+    L, n_blocks, Hkv, hd, index = _pool_shape(pool)
+    device = pool.device
+    n_seq, stride = _table_shape(table)
+    ins = (_ints("table", table, (n_seq, stride), index), _ints("pages", pages, (n_seq,), index),
+           _ints("ref", ref, (n_blocks,), index))
+    c = CompactedPages(torch.empty((n_seq, stride), dtype=torch.int32, device=device),
+                       torch.empty(n_blocks, dtype=torch.int32, device=device),
+                       torch.empty(n_blocks, dtype=torch.int32, device=device),
+                       torch.empty(1, dtype=torch.int32, device=device))
+    ws = _workspace(workspace, lib.sd2_pages_compact_workspace_bytes(n_blocks), device)
+    _check(lib, lib.sd2_pages_compact(pool.data_ptr(), L, n_blocks, Hkv, hd, ins[0], stride, ins[1], n_seq, ins[2],
+                                      c.table.data_ptr(), c.ref.data_ptr(), c.map.data_ptr(), c.n_live.data_ptr(),
+                                      ws.data_ptr(), ws.nbytes, _error_word(err, index), _stream_handle(stream, index)))
     _used_on(stream, *c, ws)
     return c
