@@ -129,48 +129,90 @@ struct ForkArgs {
   const int *table, *len, *parent, *keep, *grow, *pinned;
   int n_seq, stride, n_out;
   int *table_out, *len_out, *pages_out, *ref_out;
-  // workspace (the first three zeroed before the launch): whole holders of each page; n_out - (lowest
-  // holder of it as a partial last page), 0 for none; words: [0] CTAs done, [1] pages granted beyond
-  // which none is, [2] tail copies
-  int *count, *first, *words;
-  int4* plan;                  // per new sequence: kept pages, first granted index, granted pages, copied rows
-  int* copies;                 // the new sequences with copied tails
-  int* granted;                // page ids in order of need
+  int4* jobs;                  // workspace: tails to copy (source page, target page, rows); words[1] of them
+  int* words;                  // [0] blocks done, [1] jobs, [2] the last page granted
+  // Workspace of the plan over several blocks (the first two and `words` zeroed before it): whole holders of each
+  // page; n_out - (lowest holder of it as a partial last page), 0 for none; per new sequence its kept pages, first
+  // granted index and granted pages; the granted pages in order.
+  int *count, *first;
+  int4* plan;
+  int* granted;
   unsigned* err;
 };
 
 struct ForkSeq {
-  int parent, keep, full, tail, held, last;   // last: page id of the partial tail, -1 for none or an invalid one
+  int parent, keep, held, last;   // last: page id of a partial tail, -1 for none or an invalid one
+  __device__ __forceinline__ int full() const { return keep / kPage; }
+  __device__ __forceinline__ int tail() const { return keep % kPage; }
 };
 
 __device__ __forceinline__ ForkSeq fork_seq(const ForkArgs& a, int b) {
   ForkSeq s;
   s.parent = a.parent[b];
   const int room = a.stride * kPage;
+  const int keep = a.keep ? a.keep[b] : room, grow = a.grow ? min(max(a.grow[b], 0), room) : 0;
   int len = 0;
   if (s.parent >= 0 && s.parent < a.n_seq) len = min(max(a.len[s.parent], 0), room);
-  s.keep = a.keep ? min(max(a.keep[b], 0), len) : len;
-  s.full = s.keep / kPage;
-  s.tail = s.keep % kPage;
-  const int grow = a.grow ? min(max(a.grow[b], 0), room) : 0;
+  s.keep = min(max(keep, 0), len);
   s.held = min((s.keep + grow + kPage - 1) / kPage, a.stride);
   s.last = -1;
-  if (s.tail) {
-    const int p = a.table[static_cast<size_t>(s.parent) * a.stride + s.full];
+  if (s.tail()) {
+    const int p = a.table[static_cast<size_t>(s.parent) * a.stride + s.full()];
     if (p >= 0 && p < a.n_blocks) s.last = p;
   }
   return s;
 }
+__device__ __forceinline__ bool is_pinned(const ForkArgs& a, int p) { return a.pinned && a.pinned[p] > 0; }
 
-// A partial last page stays with a sequence if nobody holds it whole, it is not pinned and no
-// lower-numbered sequence has it as its last page: only then may the sequence append to it.
-__device__ __forceinline__ bool tail_stays(const ForkArgs& a, const ForkSeq& s, int b, const volatile int* count,
-                                           const volatile int* first) {
-  return s.last >= 0 && count[s.last] == 0 && first[s.last] == a.n_out - b && (!a.pinned || a.pinned[s.last] <= 0);
+// Counts the holders of sequence b's pages and writes the shared part of its table row (`lane` of `width` threads).
+__device__ __forceinline__ void fork_count(const ForkArgs& a, const ForkSeq& s, int b, int lane, int width, int* count,
+                                           int* first) {
+  if (lane == 0 && s.parent >= a.n_seq) raise(a.err, ERR_RANGE);
+  int* out = a.table_out + static_cast<size_t>(b) * a.stride;
+  const int full = s.full();
+  for (int i = lane; i < a.stride; i += width) {
+    int p = 0;
+    if (i < full) {
+      p = a.table[static_cast<size_t>(s.parent) * a.stride + i];
+      if (p >= 0 && p < a.n_blocks) {
+        atomicAdd(&count[p], 1);
+      } else {
+        p = 0;
+        raise(a.err, ERR_RANGE);
+      }
+    }
+    out[i] = p;
+  }
+  if (lane == 0 && s.tail()) {
+    if (s.last >= 0) atomicMax(&first[s.last], a.n_out - b);
+    else raise(a.err, ERR_RANGE);
+  }
+}
+// A partial last page stays with a sequence if nobody holds it whole, it is not pinned and no lower-numbered
+// sequence has it as its last page: only then may the sequence append to it.
+__device__ __forceinline__ bool tail_stays(const ForkArgs& a, const ForkSeq& s, int b, const int* count, const int* first) {
+  return s.last >= 0 && count[s.last] == 0 && first[s.last] == a.n_out - b && !is_pinned(a, s.last);
+}
+// What the plan settled for sequence b: kept pages, then n of the granted ones. Its table row's granted part,
+// length, page count.
+__device__ __forceinline__ void fork_grant(const ForkArgs& a, const ForkSeq& s, int b, int kept, const int* granted, int n,
+                                           int lane) {
+  int* out = a.table_out + static_cast<size_t>(b) * a.stride;
+  const bool copied = s.tail() && kept == s.full();
+  if (lane == 0) {
+    a.len_out[b] = copied && !n ? s.full() * kPage : s.keep;   // no page for the tail: cut to the whole pages
+    a.pages_out[b] = kept + n;
+    if (kept > s.full()) out[s.full()] = s.last;
+  }
+  for (int i = lane; i < n; i += 32) out[kept + i] = granted[i];
+}
+__device__ __forceinline__ int fork_ref(const ForkArgs& a, int p, int count, int first, int bound) {
+  const int r = count + (a.pinned ? max(a.pinned[p], 0) : 0);
+  return r == 0 && (first > 0 || p <= bound) ? 1 : r;
 }
 
-// Inclusive scan of one int per thread over the block (kForkThreads threads); `total` gets the sum.
-constexpr int kForkThreads = 512;
+// Inclusive scan of one int per thread over the block; `total` gets the sum.
+template <int kThreads>
 __device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   int x = v;
@@ -182,119 +224,192 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
   __syncthreads();
   if (lane == 31) warp_sums[w] = x;
   __syncthreads();
-  int before = 0;
-  total = 0;
-#pragma unroll
-  for (int i = 0; i < kForkThreads / 32; ++i) {
-    if (i < w) before += warp_sums[i];
-    total += warp_sums[i];
-  }
-  return x + before;
+  const int sums = lane < kThreads / 32 ? warp_sums[lane] : 0;
+  total = __reduce_add_sync(0xffffffffu, sums);
+  return x + __reduce_add_sync(0xffffffffu, lane < w ? sums : 0);
 }
 
-// Counts holders and writes the shared part of the tables, one new sequence per CTA at a time; the
-// CTA that finishes last decides who keeps a tail and which free pages are granted.
+// The whole plan in one block, everything counted in shared memory: batches and pools up to the limits below.
+// (A block over several has to be told that the others are done and needs its counters zeroed by a launch of
+// its own: one prompt forked into four, pool of 1B-shaped layers, 19.9 us that way.)
+constexpr int kOneThreads = 1024, kOneSeqs = 2048, kOnePages = 12288, kOneEntries = 1 << 16;
+constexpr size_t one_block_smem(int n_out, int n_blocks) {
+  return static_cast<size_t>(n_out) * (sizeof(ForkSeq) + sizeof(int2)) + static_cast<size_t>(n_blocks) * 12;
+}
+__global__ void __launch_bounds__(kOneThreads) fork_one_block_kernel(const ForkArgs a) {
+  pdl_trigger();               // (launched after everything before it has completed)
+  extern __shared__ int4 shared[];
+  ForkSeq* seqs = reinterpret_cast<ForkSeq*>(shared);
+  int2* kept_from = reinterpret_cast<int2*>(seqs + a.n_out);   // kept pages, first granted index
+  int* count = reinterpret_cast<int*>(kept_from + a.n_out);
+  int *first = count + a.n_blocks, *granted = first + a.n_blocks;
+  __shared__ int sums[kOneThreads / 32];
+  __shared__ int n_jobs, bound;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    n_jobs = 0;
+    bound = -1;
+  }
+  for (int b = threadIdx.x; b < a.n_out; b += kOneThreads) seqs[b] = fork_seq(a, b);
+  for (int p = threadIdx.x; p < 2 * a.n_blocks; p += kOneThreads) count[p] = 0;
+  __syncthreads();
+  for (int b = warp; b < a.n_out; b += kOneThreads / 32) fork_count(a, seqs[b], b, lane, 32, count, first);
+  __syncthreads();
+  // who needs how many pages, in the order of the sequences (two per thread at most)
+  int need = 0, kept[2] = {0, 0}, want[2] = {0, 0}, start[2] = {0, 0};
+#pragma unroll
+  for (int k = 0; k < kOneSeqs / kOneThreads; ++k) {
+    const int b = k * kOneThreads + threadIdx.x;
+    if (k * kOneThreads >= a.n_out) break;
+    if (b < a.n_out) {
+      kept[k] = seqs[b].full() + tail_stays(a, seqs[b], b, count, first);
+      want[k] = seqs[b].held - kept[k];
+    }
+    int total;
+    start[k] = need + block_scan<kOneThreads>(want[k], sums, total) - want[k];
+    need += total;
+  }
+  // the lowest free pages, until the need is met
+  int found = 0;
+  for (int p0 = 0; p0 < a.n_blocks && found < need; p0 += kOneThreads) {
+    const int p = p0 + threadIdx.x;
+    const bool free = p < a.n_blocks && count[p] == 0 && first[p] == 0 && !is_pinned(a, p);
+    int total;
+    const int at = found + block_scan<kOneThreads>(free, sums, total) - 1;
+    if (free && at < need) {
+      granted[at] = p;
+      if (at == need - 1) bound = p;
+    }
+    found += total;
+  }
+  if (found < need) {          // every free page went
+    if (threadIdx.x == 0) {
+      bound = a.n_blocks - 1;
+      raise(a.err, ERR_PAGES);
+    }
+  }
+  found = min(found, need);
+  __syncthreads();
+  // the jobs' order does not matter: their pages are distinct
+#pragma unroll
+  for (int k = 0; k < kOneSeqs / kOneThreads; ++k) {
+    const int b = k * kOneThreads + threadIdx.x;
+    if (b >= a.n_out) break;
+    const ForkSeq s = seqs[b];
+    const int n = min(max(found - start[k], 0), want[k]);
+    if (s.tail() && kept[k] == s.full() && n && s.last >= 0)
+      a.jobs[atomicAdd(&n_jobs, 1)] = make_int4(s.last, granted[start[k]], s.tail(), 0);
+    kept_from[b] = make_int2(kept[k], start[k]);
+  }
+  __syncthreads();
+  for (int b = warp; b < a.n_out; b += kOneThreads / 32) {
+    const int2 k = kept_from[b];
+    fork_grant(a, seqs[b], b, k.x, granted + k.y, min(max(found - k.y, 0), seqs[b].held - k.x), lane);
+  }
+  for (int p = threadIdx.x; p < a.n_blocks; p += kOneThreads) a.ref_out[p] = fork_ref(a, p, count[p], first[p], bound);
+  if (threadIdx.x == 0) a.words[1] = n_jobs;
+}
+
+// Any size: one new sequence per block at a time; the block that finishes last decides who keeps a tail and
+// which free pages are granted.
+constexpr int kForkThreads = 512;
 __global__ void __launch_bounds__(kForkThreads) fork_plan_kernel(const ForkArgs a) {
   pdl_trigger();               // (launched after everything before it has completed)
   __shared__ int sums[kForkThreads / 32];
-  __shared__ int last_cta;
-  for (int b = blockIdx.x; b < a.n_out; b += gridDim.x) {
-    const ForkSeq s = fork_seq(a, b);
-    if (threadIdx.x == 0 && s.parent >= a.n_seq) raise(a.err, ERR_RANGE);
-    int* out = a.table_out + static_cast<size_t>(b) * a.stride;
-    for (int i = threadIdx.x; i < a.stride; i += kForkThreads) {
-      int p = 0;
-      if (i < s.full) {
-        p = a.table[static_cast<size_t>(s.parent) * a.stride + i];
-        if (p >= 0 && p < a.n_blocks) {
-          atomicAdd(&a.count[p], 1);
-        } else {
-          p = 0;
-          raise(a.err, ERR_RANGE);
-        }
-      }
-      out[i] = p;
-    }
-    if (threadIdx.x == 0 && s.tail) {
-      if (s.last >= 0) atomicMax(&a.first[s.last], a.n_out - b);
-      else raise(a.err, ERR_RANGE);
-    }
-  }
+  __shared__ int last_cta, bound;
+  for (int b = blockIdx.x; b < a.n_out; b += gridDim.x)
+    fork_count(a, fork_seq(a, b), b, threadIdx.x, kForkThreads, a.count, a.first);
   __threadfence();
   __syncthreads();
   if (threadIdx.x == 0) last_cta = atomicAdd(&a.words[0], 1) == static_cast<int>(gridDim.x) - 1;
   __syncthreads();
   if (!last_cta) return;
   __threadfence();
-  const volatile int *count = a.count, *first = a.first;
-  // who needs how many pages: their order is that of the sequences
-  int need = 0, n_copies = 0;
+  int need = 0;
   for (int b0 = 0; b0 < a.n_out; b0 += kForkThreads) {
     const int b = b0 + threadIdx.x;
-    int want = 0, copy = 0, kept = 0, rows = 0;
+    int want = 0, kept = 0;
     if (b < a.n_out) {
       const ForkSeq s = fork_seq(a, b);
-      const bool stays = tail_stays(a, s, b, count, first);
-      kept = s.full + (stays ? 1 : 0);
+      kept = s.full();
+      if (s.last >= 0)
+        kept += __ldcg(a.count + s.last) == 0 && __ldcg(a.first + s.last) == a.n_out - b && !is_pinned(a, s.last);
       want = s.held - kept;
-      copy = s.tail > 0 && !stays;
-      rows = copy ? s.tail : 0;
     }
-    int total, copies;
-    const int end = block_scan(want, sums, total);
-    const int cend = block_scan(copy, sums, copies);
-    if (b < a.n_out) a.plan[b] = make_int4(kept, need + end - want, want, rows);
-    if (copy) a.copies[n_copies + cend - 1] = b;
+    int total;
+    const int end = block_scan<kForkThreads>(want, sums, total);
+    if (b < a.n_out) a.plan[b] = make_int4(kept, need + end - want, want, 0);
     need += total;
-    n_copies += copies;
   }
-  // the lowest free pages, until the need is met
+  // the lowest free pages, until the need is met; a thread looks at 16 in a row (the arrays are padded to that)
   constexpr int kPer = 16;
-  int found = 0, bound = -1;
-  __shared__ int top;
+  if (threadIdx.x == 0) bound = -1;
+  int found = 0;
   for (int p0 = 0; p0 < a.n_blocks && found < need; p0 += kForkThreads * kPer) {
     const int lo = p0 + threadIdx.x * kPer;
     unsigned mask = 0;
+    if (lo < a.n_blocks) {
+      int4 c[kPer / 4], f[kPer / 4];
+      int pin[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (lo + i < a.n_blocks && count[lo + i] == 0 && first[lo + i] == 0 && (!a.pinned || a.pinned[lo + i] <= 0))
-        mask |= 1u << i;
-    int total;
-    int at = found + block_scan(__popc(mask), sums, total) - __popc(mask);
-    if (threadIdx.x == 0) top = -1;
-    __syncthreads();
-    for (; mask; mask &= mask - 1) {
-      if (at < need) {
-        const int p = lo + __ffs(mask) - 1;
-        a.granted[at] = p;
-        atomicMax(&top, p);
+      for (int i = 0; i < kPer / 4; ++i) {
+        c[i] = __ldcg(reinterpret_cast<const int4*>(a.count + lo) + i);
+        f[i] = __ldcg(reinterpret_cast<const int4*>(a.first + lo) + i);
       }
-      ++at;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) pin[i] = a.pinned && lo + i < a.n_blocks ? a.pinned[lo + i] : 0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int4 cv = c[i / 4], fv = f[i / 4];
+        const int x = i % 4 == 0 ? cv.x | fv.x : i % 4 == 1 ? cv.y | fv.y : i % 4 == 2 ? cv.z | fv.z : cv.w | fv.w;
+        if (lo + i < a.n_blocks && x == 0 && pin[i] <= 0) mask |= 1u << i;
+      }
     }
-    __syncthreads();
-    bound = max(bound, top);
+    int total;
+    int at = found + block_scan<kForkThreads>(__popc(mask), sums, total) - __popc(mask);
+    for (; mask && at < need; mask &= mask - 1, ++at) {
+      const int p = lo + __ffs(mask) - 1;
+      a.granted[at] = p;
+      if (at == need - 1) bound = p;
+    }
     found += total;
+  }
+  if (found < need && threadIdx.x == 0) {   // every free page went
+    bound = a.n_blocks - 1;
+    raise(a.err, ERR_PAGES);
   }
   found = min(found, need);
   __syncthreads();
-  for (int b = threadIdx.x; b < a.n_out; b += kForkThreads) {
-    int4 p = a.plan[b];
-    p.z = min(max(found - p.y, 0), p.z);
-    a.plan[b] = p;
+  int n_jobs = 0;
+  for (int b0 = 0; b0 < a.n_out; b0 += kForkThreads) {
+    const int b = b0 + threadIdx.x;
+    bool copy = false;
+    int4 p = make_int4(0, 0, 0, 0);
+    ForkSeq s{};
+    if (b < a.n_out) {
+      p = a.plan[b];
+      s = fork_seq(a, b);
+      p.z = min(max(found - p.y, 0), p.z);
+      a.plan[b] = p;
+      copy = s.tail() && p.x == s.full() && p.z && s.last >= 0;
+    }
+    int total;
+    const int at = n_jobs + block_scan<kForkThreads>(copy, sums, total) - 1;
+    if (copy) a.jobs[at] = make_int4(s.last, a.granted[p.y], s.tail(), 0);
+    n_jobs += total;
   }
   if (threadIdx.x == 0) {
-    a.words[1] = bound;
-    a.words[2] = n_copies;
-    if (found < need) raise(a.err, ERR_PAGES);
+    a.words[1] = n_jobs;
+    a.words[2] = bound;
   }
 }
 
 constexpr int kCopyThreads = 256, kCopyPer = 8;
 
 // Copies 16-byte vectors [i0, i0 + kCopyThreads * kCopyPer) of page src to page dst, numbered through
-// the page's L blocks of `per_layer` vectors; of each 16-row panel only the first `rows` rows.
-__device__ __forceinline__ void copy_vectors(uint4* pool, long long layer_stride, int per_layer, int vec_row, int src,
-                                             int dst, int rows, int i0, int n) {
+// the page's L blocks of `per_layer` vectors.
+__device__ __forceinline__ void copy_vectors(uint4* pool, long long layer_stride, int per_layer, int src, int dst, int i0,
+                                             int n) {
   uint4 x[kCopyPer];
   long long at[kCopyPer];
 #pragma unroll
@@ -303,11 +418,9 @@ __device__ __forceinline__ void copy_vectors(uint4* pool, long long layer_stride
     at[u] = -1;
     if (i < n) {
       const int l = i / per_layer, j = i - l * per_layer;
-      if ((j / vec_row) % kPage < rows) {
-        const long long base = l * layer_stride + j;
-        x[u] = ld_once(pool + base + static_cast<long long>(src) * per_layer);
-        at[u] = base + static_cast<long long>(dst) * per_layer;
-      }
+      const long long base = l * layer_stride + j;
+      x[u] = ld_once(pool + base + static_cast<long long>(src) * per_layer);
+      at[u] = base + static_cast<long long>(dst) * per_layer;
     }
   }
 #pragma unroll
@@ -315,38 +428,46 @@ __device__ __forceinline__ void copy_vectors(uint4* pool, long long layer_stride
     if (at[u] >= 0) pool[at[u]] = x[u];
 }
 
-// Writes what the plan decided (granted table entries, lengths, page counts, reference counts) and
-// copies the tails.
-__global__ void __launch_bounds__(kCopyThreads) fork_write_kernel(const ForkArgs a) {
+// Copies the tails: of each of a page's L x 2 x Hkv panels of 16 rows the first `rows`. A warp takes two panels
+// at a time. Where the plan ran over several blocks (`finish`), writes what it settled, too.
+__global__ void __launch_bounds__(kCopyThreads) fork_copy_kernel(const ForkArgs a, int finish) {
   pdl_wait();
-  const int tid = blockIdx.x * kCopyThreads + threadIdx.x, n_thr = gridDim.x * kCopyThreads;
-  const int bound = a.words[1], n_copies = a.words[2];
   const int lane = threadIdx.x & 31;
-  for (int b = tid >> 5; b < a.n_out; b += n_thr >> 5) {   // a warp per sequence
-    const ForkSeq s = fork_seq(a, b);
-    const int4 p = a.plan[b];
-    int* out = a.table_out + static_cast<size_t>(b) * a.stride;
-    if (lane == 0) {
-      a.len_out[b] = p.w && !p.z ? s.full * kPage : s.keep;   // no page for the tail: cut to the full pages
-      a.pages_out[b] = p.x + p.z;
-      if (p.x > s.full) out[s.full] = s.last;
+  const int tid = blockIdx.x * kCopyThreads + threadIdx.x, n_thr = gridDim.x * kCopyThreads;
+  const int n_jobs = a.words[1];
+  if (finish) {
+    const int bound = a.words[2];
+    for (int b = tid >> 5; b < a.n_out; b += n_thr >> 5) {
+      const int4 p = a.plan[b];
+      fork_grant(a, fork_seq(a, b), b, p.x, a.granted + p.y, p.z, lane);
     }
-    for (int i = lane; i < p.z; i += 32) out[p.x + i] = a.granted[p.y + i];
+    for (int p = tid; p < a.n_blocks; p += n_thr) a.ref_out[p] = fork_ref(a, p, a.count[p], a.first[p], bound);
   }
-  for (int p = tid; p < a.n_blocks; p += n_thr) {
-    int r = a.count[p] + (a.pinned ? max(a.pinned[p], 0) : 0);
-    if (r == 0 && (a.first[p] > 0 || p <= bound)) r = 1;
-    a.ref_out[p] = r;
-  }
-  const int vec_row = a.hd / 8, per_layer = 2 * a.Hkv * kPage * vec_row;
-  const int n = a.L * per_layer, per_cta = kCopyThreads * kCopyPer, parts = (n + per_cta - 1) / per_cta;
-  for (long long w = blockIdx.x; w < static_cast<long long>(n_copies) * parts; w += gridDim.x) {
-    const int b = a.copies[w / parts];
-    const int4 p = a.plan[b];
-    const ForkSeq s = fork_seq(a, b);
-    if (!p.z || s.last < 0) continue;
-    copy_vectors(reinterpret_cast<uint4*>(a.pool), static_cast<long long>(a.n_blocks) * per_layer, per_layer, vec_row,
-                 s.last, a.granted[p.y], p.w, static_cast<int>(w % parts) * per_cta, n);
+  const int vec_row = a.hd / 8, panels = 2 * a.Hkv, pairs = (a.L * panels + 1) / 2;
+  const long long panel = static_cast<long long>(kPage) * vec_row, layer = static_cast<long long>(a.n_blocks) * panels * panel;
+  uint4* pool = reinterpret_cast<uint4*>(a.pool);
+  for (long long w = tid >> 5; w < static_cast<long long>(n_jobs) * pairs; w += n_thr >> 5) {
+    const int4 job = a.jobs[w / pairs];
+    const int first = 2 * static_cast<int>(w % pairs), n = job.z * vec_row;
+    for (int i0 = lane; i0 < n; i0 += 32 * kCopyPer) {
+      uint4 x[2][kCopyPer];
+      uint4* to[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int l = (first + k) / panels, h = (first + k) % panels;
+        const long long at = l * layer + h * panel;
+        const uint4* from = pool + at + static_cast<long long>(job.x) * panels * panel;
+        to[k] = pool + at + static_cast<long long>(job.y) * panels * panel;
+#pragma unroll
+        for (int u = 0; u < kCopyPer; ++u)
+          if (l < a.L && i0 + 32 * u < n) x[k][u] = ld_once(from + i0 + 32 * u);
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int u = 0; u < kCopyPer; ++u)
+          if (first + k < a.L * panels && i0 + 32 * u < n) to[k][i0 + 32 * u] = x[k][u];
+    }
   }
 }
 
@@ -445,12 +566,12 @@ __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const Compac
     }
     a.table_out[e] = to;
   }
-  const int vec_row = a.hd / 8, per_layer = 2 * a.Hkv * kPage * vec_row;
+  const int per_layer = 2 * a.Hkv * kPage * (a.hd / 8);
   const int n = a.L * per_layer, per_cta = kCopyThreads * kCopyPer, parts = (n + per_cta - 1) / per_cta;
   for (long long w = blockIdx.x; w < static_cast<long long>(n_move) * parts; w += gridDim.x) {
     const int j = static_cast<int>(w / parts);
-    copy_vectors(reinterpret_cast<uint4*>(a.pool), static_cast<long long>(a.n_blocks) * per_layer, per_layer, vec_row,
-                 a.movers[j], a.holes[j], kPage, static_cast<int>(w % parts) * per_cta, n);
+    copy_vectors(reinterpret_cast<uint4*>(a.pool), static_cast<long long>(a.n_blocks) * per_layer, per_layer, a.movers[j],
+                 a.holes[j], static_cast<int>(w % parts) * per_cta, n);
   }
 }
 
@@ -513,8 +634,8 @@ sd2_status sd2_pages_append(const void* d_k, int64_t ldk, const void* d_v, int64
 
 size_t sd2_pages_fork_workspace_bytes(int32_t n_out, int32_t n_blocks) {
   if (n_out < 1 || n_blocks < 1) return 0;
-  const size_t n = n_out, p = n_blocks;
-  return round_up(n * 16 + (3 * p + 4 + n) * 4, 256);
+  const size_t n = n_out, p = round_up(n_blocks, 16);
+  return round_up(2 * n * 16 + (3 * p + 4) * 4, 256);   // jobs and plan; counts, granted pages and words
 }
 
 sd2_status sd2_pages_fork(void* d_pool, int32_t L, int32_t n_blocks, int32_t Hkv, int32_t hd, const int32_t* d_table,
@@ -537,19 +658,32 @@ sd2_status sd2_pages_fork(void* d_pool, int32_t L, int32_t n_blocks, int32_t Hkv
   a.table = d_table; a.len = d_len; a.parent = d_parent; a.keep = d_keep; a.grow = d_grow; a.pinned = d_pinned;
   a.n_seq = n_seq; a.stride = bt_stride; a.n_out = n_out;
   a.table_out = d_table_out; a.len_out = d_len_out; a.pages_out = d_pages_out; a.ref_out = d_ref_out; a.err = d_err;
-  a.plan = static_cast<int4*>(d_workspace);
+  const size_t padded = round_up(n_blocks, 16);
+  a.jobs = static_cast<int4*>(d_workspace);
+  a.plan = a.jobs + n_out;
   a.count = reinterpret_cast<int*>(a.plan + n_out);
-  a.first = a.count + n_blocks;
-  a.words = a.first + n_blocks;
+  a.first = a.count + padded;
+  a.words = a.first + padded;
   a.granted = a.words + 4;
-  a.copies = a.granted + n_blocks;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = cudaMemsetAsync(a.count, 0, (2 * static_cast<size_t>(n_blocks) + 4) * sizeof(int), st);
-  if (e != cudaSuccess) return launched(e, "fork workspace");
   const int sms = sm_count_cached();
-  fork_plan_kernel<<<std::min(n_out, 2 * sms), kForkThreads, 0, st>>>(a);
+  const bool one = n_out <= kOneSeqs && n_blocks <= kOnePages && static_cast<int64_t>(n_out) * bt_stride <= kOneEntries;
+  cudaError_t e;
+  if (one) {
+    const size_t smem = one_block_smem(n_out, n_blocks);
+    if (smem > 48 * 1024) {
+      e = cudaFuncSetAttribute(fork_one_block_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(one_block_smem(kOneSeqs, kOnePages)));
+      if (e != cudaSuccess) return launched(e, "fork plan");
+    }
+    fork_one_block_kernel<<<1, kOneThreads, smem, st>>>(a);
+  } else {
+    e = cudaMemsetAsync(a.count, 0, (2 * padded + 4) * sizeof(int), st);
+    if (e != cudaSuccess) return launched(e, "fork workspace");
+    fork_plan_kernel<<<std::min(n_out, 2 * sms), kForkThreads, 0, st>>>(a);
+  }
   if ((e = cudaGetLastError()) != cudaSuccess) return launched(e, "fork plan launch");
-  return launched(launch_pdl(fork_write_kernel, dim3(8 * sms), dim3(kCopyThreads), 0, st, a), "fork launch");
+  return launched(launch_pdl(fork_copy_kernel, dim3(4 * sms), dim3(kCopyThreads), 0, st, a, one ? 0 : 1), "fork launch");
 }
 
 size_t sd2_pages_compact_workspace_bytes(int32_t n_blocks) {
