@@ -322,6 +322,11 @@ sd2_status sd2_set_gemm_impl(sd2_ctx* ctx, int32_t impl);
  * arithmetic of a2. Only with the tensor-core GEMM (sd2_set_gemm_impl 0). Drops captured graphs. */
 sd2_status sd2_set_drafter_chain(sd2_ctx* ctx, int32_t enable);
 
+/* Read prompts (sd2_prefill, sd2_generate) through the prompt attention kernel of sd2_attention_prompt (1: tensor
+ * cores, 256 query vectors per K/V tile) or through the decode kernel, at most 64 query vectors at a time (0, the
+ * default). The same arithmetic of the prefill up to rounding; takes effect with the next prefill. */
+sd2_status sd2_set_prompt_attention(sd2_ctx* ctx, int32_t enable);
+
 /* Decode steps of one sequence (batch 1): run each layer's attention inside its O projection
  * (1, where the model allows it: head dim 64, 2..8 KV heads, rows x heads per KV head <= 16,
  * context <= 4096, the projection's tiles x KV heads <= the SM count) or as a kernel of its own

@@ -66,6 +66,7 @@ struct Plan {
   // decode steps: the pre-step lengths attention may read before its programmatic wait (AttnArgs)
   const int* pre_len = nullptr;
   int pre_stable = 0, pre_fresh = 0;
+  const int *cu = nullptr, *kv_len = nullptr;   // prompts for the prompt attention kernel: row offsets, lengths
 };
 
 struct ProfRec {
@@ -109,6 +110,7 @@ struct sd2_ctx {
   ChainPlan chain{};             // the drafter's persistent layer chain (chain.cu), when its shape allows
   bool chain_ok = false;
   bool use_chain = false;        // measured slower than the per-kernel path on GB300 (off by default)
+  bool prompt_attn = false;      // prompts through the prompt attention kernel (sd2_set_prompt_attention)
   bool attn_in_o = false;        // decode attention inside the O projection: measured slower on GB300 (off by default)
   void *a = nullptr, *attn = nullptr, *h = nullptr, *g_bf = nullptr, *hml_in = nullptr;
   // long-context attention: partials of the context clusters and the per-share arrival counters
@@ -506,6 +508,15 @@ sd2_status forward(sd2_ctx* c, const Model& m, const Plan& p, const FwdOut& o) {
       }
     }
     if (fused) parts = gemm_norm_parts(go);
+    const bool whole_prompts = c->prompt_attn && p.cu;   // prefill rows, by the prompt kernel
+    if (whole_prompts) {
+      // the q|k|v rows have been rotated and appended: their memory holds the bf16 queries
+      CK(timed(c, PC_OTHER, 0, [&] { return rows_to_bf16(c->q, H * hd, M, H * hd, c->qkv, c->st); }));
+      PromptAttnArgs pa{};
+      pa.q = c->qkv; pa.ldq = static_cast<long long>(H) * hd; pa.M = M; pa.H = H; pa.kv = m.cache(); pa.layer = l;
+      pa.cu = p.cu; pa.kv_len = p.kv_len; pa.n_seq = c->B; pa.max_kv = p.chunk; pa.out = c->attn; pa.err = c->errw;
+      CK(timed(c, PC_ATTN, 0, [&] { return prompt_attention(pa, c->st); }));
+    }
     AttnArgs at{};
     at.q = c->q; at.kv = m.cache(); at.layer = l; at.row_pos = p.pos;
     at.grp_row0 = p.g_row0; at.grp_nrows = p.g_nrows; at.grp_seq = p.g_seq; at.n_groups = p.n_groups;
@@ -578,7 +589,7 @@ sd2_status forward(sd2_ctx* c, const Model& m, const Plan& p, const FwdOut& o) {
     if (in_o)
       RUN_GEMM(go, gemm_bytes(M, d, H * hd, 8) + kvb);
     else {
-      CK(timed(c, PC_ATTN, kvb, [&] { return attention(at, c->st); }));
+      if (!whole_prompts) CK(timed(c, PC_ATTN, kvb, [&] { return attention(at, c->st); }));
       RUN_GEMM(go, gemm_bytes(M, d, H * hd, 8));
     }
     if (!fused)
@@ -830,7 +841,7 @@ sd2_status sd2_init(const sd2_config* cfg, const sd2_weights* w, void* stream, s
     ALLOC(c->temp, maxB);
     ALLOC(c->errw, 1);
     ALLOC(c->row_tok, R); ALLOC(c->row_pos, R); ALLOC(c->row_seq, R); ALLOC(c->row_valid, R);
-    c->statics_cap = 8 * R + 64;
+    c->statics_cap = 8 * R + 64 + maxB;
     ALLOC(c->statics, c->statics_cap);
     ALLOC(c->x, static_cast<size_t>(R) * dmax);
     ALLOC(c->a, static_cast<size_t>(R) * dmax * 2);
@@ -987,6 +998,9 @@ sd2_status sd2_prefill(sd2_ctx* c, int32_t batch, const int32_t* d_tokens, const
   const int o_dr0 = push(dr0), o_dnr = push(dnr), o_dsq = push(dsq);
   std::vector<int> cu(h_cu_lens, h_cu_lens + batch + 1);
   const int o_cu = push(cu);
+  std::vector<int> lens;               // cached length of each prompt: its own rows
+  for (int b = 0; b < batch && c->prompt_attn; ++b) lens.push_back(h_cu_lens[b + 1] - h_cu_lens[b]);
+  const int o_len = push(lens);
   if ((int)st.size() > c->statics_cap) {
     drop_graphs(c);
     c->graph_key.clear();
@@ -1002,6 +1016,7 @@ sd2_status sd2_prefill(sd2_ctx* c, int32_t batch, const int32_t* d_tokens, const
   pv.M = total; pv.tok = d_tokens; pv.pos = S + o_pos; pv.seq = S + o_seq; pv.valid = S + o_valid;
   pv.n_groups = (int)vr0.size(); pv.g_row0 = S + o_vr0; pv.g_nrows = S + o_vnr; pv.g_seq = S + o_vsq;
   pv.n_splits = 1; pv.chunk = ((maxlen + 63) / 64) * 64; pv.max_rows = std::min(maxlen, c->V.group_rows());
+  if (c->prompt_attn) { pv.cu = S + o_cu; pv.kv_len = S + o_len; }
   Plan pd = pv;
   pd.n_groups = (int)dr0.size(); pd.g_row0 = S + o_dr0; pd.g_nrows = S + o_dnr; pd.g_seq = S + o_dsq;
   pd.max_rows = std::min(maxlen, c->D.group_rows());
@@ -1172,6 +1187,12 @@ sd2_status sd2_set_fused_attention(sd2_ctx* c, int32_t enable) {
   if (!c) return fail(nullptr, SD2_EINVAL, "null context");
   c->attn_in_o = enable != 0;
   drop_graphs(c);
+  return SD2_OK;
+}
+
+sd2_status sd2_set_prompt_attention(sd2_ctx* c, int32_t enable) {
+  if (!c) return fail(nullptr, SD2_EINVAL, "null context");
+  c->prompt_attn = enable != 0;        // (the prefill is not part of a captured graph)
   return SD2_OK;
 }
 

@@ -243,6 +243,25 @@ int attention_ctas_per_sm(int hd);
 // clusters pack into the GPCs where the per-SM count above does not. 0 for shapes attention() rejects.
 int attention_max_clusters(const AttnArgs& a);
 
+// Causal attention of packed prompt rows over the paged cache (prompt_attention.cu): rows cu[s] .. cu[s+1] - 1 are
+// the last positions of sequence s, the last of them at kv_len[s] - 1. Without `work` (prompt_attention_work_bytes)
+// the positions are not split.
+struct PromptAttnArgs {
+  const void* q;         // bf16, row m's heads at q + m * ldq
+  long long ldq;
+  int M, H;
+  KVCache kv;
+  int layer;
+  const int *cu, *kv_len;
+  int n_seq, max_kv;
+  void* out;             // [M, H * hd] bf16
+  float* lse;            // [M, H] or null
+  void* work;
+  unsigned* err;         // ERR_TIMEOUT, ERR_RANGE (a page id outside the pool); not null
+};
+size_t prompt_attention_work_bytes(int M, int n_seq, int H, int Hkv, int hd, int max_kv);
+cudaError_t prompt_attention(const PromptAttnArgs& p, cudaStream_t st);
+
 // ---------------------------------------------------------------- persistent layer chain
 // Every decoder layer of one forward pass over at most 16 token rows in one cooperative launch
 // (chain.cu): the projections stream their weights through one TMA ring across grid-wide

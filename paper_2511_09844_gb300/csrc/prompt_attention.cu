@@ -973,12 +973,6 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant_
   if (a.lse && lane == 0) a.lse[item] = total > 0.f ? (mx + log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
-sd2_status fail(sd2_status s, const std::string& m) {
-  record_last_error(m);
-  return s;
-}
-bool unaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
-
 // The grid: query tiles (an upper bound: the sequences' lengths are on the device), and splits of the
 // positions where tiles x KV heads leave SMs idle. A split keeps at least two K/V tiles (one row on 1000
 // positions: 12.7 us with two, 14.9 with four, 19.1 with eight), and as many that the partial results, f32,
@@ -1021,6 +1015,41 @@ cudaError_t launch(const PromptArgs& a, int tiles, cudaStream_t st) {
 }
 
 }  // namespace
+
+size_t prompt_attention_work_bytes(int M, int n_seq, int H, int Hkv, int hd, int max_kv) {
+  const int splits = shape_of(M, n_seq, H, Hkv, hd, max_kv).splits;
+  return splits > 1 ? static_cast<size_t>(2 * splits) * M * H * (hd + 1) * 4 : 0;
+}
+
+cudaError_t prompt_attention(const PromptAttnArgs& p, cudaStream_t st) {
+  if (p.M <= 0) return cudaSuccess;
+  const int hd = p.kv.hd, Hkv = p.kv.Hkv;
+  const Shape s = shape_of(p.M, p.n_seq, p.H, Hkv, hd, p.max_kv);
+  PromptArgs a{};
+  a.M = p.M; a.H = p.H; a.Hkv = Hkv; a.G = s.G; a.T = s.T; a.n_blocks = p.kv.n_blocks; a.bt_stride = p.kv.bt_stride;
+  a.n_seq = p.n_seq; a.n_splits = p.work ? s.splits : 1; a.kv_rows = p.kv.n_blocks * 2 * Hkv * kPage;
+  a.table = p.kv.table; a.cu = p.cu; a.kv_len = p.kv_len; a.out = static_cast<bf16*>(p.out); a.lse = p.lse; a.err = p.err;
+  a.part_o = static_cast<float*>(p.work);
+  a.part_lse = a.part_o + static_cast<size_t>(2 * a.n_splits) * p.M * p.H * hd;
+  a.pool = static_cast<const bf16*>(p.kv.pool) + static_cast<size_t>(p.layer) * p.kv.n_blocks * 2 * Hkv * kPage * hd;
+  // Q: [row][head][hd], boxes of T rows x G heads x 64; K: [page row][hd], a page x 64; V: a page x all of hd,
+  // one 64-column half behind the other
+  const long long kv_rows = a.kv_rows;
+  if (!encode_map3(&a.map_q, p.q, {hd, p.H, p.M}, {hd, p.ldq}, {64, s.G, s.T}) ||
+      !encode_map3(&a.map_k, a.pool, {hd, kv_rows, 1}, {hd, kv_rows * hd}, {64, kPage, 1}) ||
+      !encode_map3(&a.map_v, a.pool, {64, kv_rows, hd / 64}, {hd, 64}, {64, kPage, hd / 64}))
+    return cudaErrorInvalidValue;
+  return hd == 64 ? launch<64>(a, s.tiles, st) : launch<128>(a, s.tiles, st);
+}
+
+namespace {
+sd2_status fail(sd2_status s, const std::string& m) {
+  record_last_error(m);
+  return s;
+}
+bool unaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
+
+}  // namespace
 }  // namespace sd2
 
 extern "C" {
@@ -1029,9 +1058,8 @@ using namespace sd2;
 
 size_t sd2_attention_prompt_workspace_bytes(int32_t M, int32_t n_seq, int32_t H, int32_t Hkv, int32_t hd, int32_t max_kv) {
   if (M < 1 || n_seq < 1 || Hkv < 1 || H < Hkv || H % Hkv || (hd != 64 && hd != 128) || max_kv < 1) return 0;
-  const Shape s = shape_of(M, n_seq, H, Hkv, hd, max_kv);
-  const size_t parts = s.splits > 1 ? static_cast<size_t>(2 * s.splits) * M * H * (hd + 1) * 4 : 0;
-  return 256 + (parts + 255) / 256 * 256;
+  // a stand-in for the error word, then the splits' partial results
+  return 256 + (prompt_attention_work_bytes(M, n_seq, H, Hkv, hd, max_kv) + 255) / 256 * 256;
 }
 
 sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t H, int32_t Hkv, int32_t hd,
@@ -1053,26 +1081,15 @@ sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t
     return fail(SD2_EINVAL, "workspace too small");
   if (unaligned(d_workspace, 256)) return fail(SD2_EINVAL, "workspace not 256-byte aligned");
   if (M == 0) return SD2_OK;
-  const Shape s = shape_of(M, n_seq, H, Hkv, hd, max_kv);
-  PromptArgs a{};
-  a.M = M; a.H = H; a.Hkv = Hkv; a.G = s.G; a.T = s.T; a.n_blocks = n_blocks; a.bt_stride = bt_stride;
-  a.n_seq = n_seq; a.n_splits = s.splits; a.kv_rows = n_blocks * 2 * Hkv * kPage;
-  a.table = d_table; a.cu = d_cu_rows; a.kv_len = d_kv_len; a.out = static_cast<bf16*>(d_out); a.lse = d_lse;
-  // the workspace: a stand-in for the error word, then the splits' partial results
-  a.err = d_err ? d_err : static_cast<unsigned*>(d_workspace);
-  a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(d_workspace) + 256);
-  a.part_lse = a.part_o + static_cast<size_t>(2 * s.splits) * M * H * hd;
-  const bf16* pool = static_cast<const bf16*>(d_pool) + static_cast<size_t>(layer) * n_blocks * 2 * Hkv * kPage * hd;
-  a.pool = pool;
-  // Q: [row][head][hd], boxes of T rows x G heads x 64; K: [page row][hd], a page x 64; V: a page x all of hd,
-  // one 64-column half behind the other
-  const long long kv_rows = a.kv_rows;
-  if (!encode_map3(&a.map_q, d_q, {hd, H, M}, {hd, ldq}, {64, s.G, s.T}) ||
-      !encode_map3(&a.map_k, pool, {hd, kv_rows, 1}, {hd, kv_rows * hd}, {64, kPage, 1}) ||
-      !encode_map3(&a.map_v, pool, {64, kv_rows, hd / 64}, {hd, 64}, {64, kPage, hd / 64}))
-    return fail(SD2_ECUDA, "prompt attention: tensor map");
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = hd == 64 ? launch<64>(a, s.tiles, st) : launch<128>(a, s.tiles, st);
+  PromptAttnArgs p{};
+  p.q = d_q; p.ldq = ldq; p.M = M; p.H = H;
+  p.kv.pool = const_cast<void*>(d_pool); p.kv.table = d_table; p.kv.bt_stride = bt_stride; p.kv.n_blocks = n_blocks;
+  p.kv.Hkv = Hkv; p.kv.hd = hd;
+  p.layer = layer; p.cu = d_cu_rows; p.kv_len = d_kv_len; p.n_seq = n_seq; p.max_kv = max_kv;
+  p.out = d_out; p.lse = d_lse;
+  p.work = static_cast<unsigned char*>(d_workspace) + 256;
+  p.err = d_err ? d_err : static_cast<unsigned*>(d_workspace);
+  const cudaError_t e = prompt_attention(p, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? SD2_OK : fail(SD2_ECUDA, std::string("prompt attention launch: ") + cudaGetErrorString(e));
 }
 

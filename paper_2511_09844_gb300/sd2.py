@@ -32,7 +32,8 @@ EXPORTS = ["sd2_init", "sd2_prefill", "sd2_step", "sd2_accept", "sd2_check", "sd
            "sd2_accept_logits_noalloc_check", "sd2_debug_fail_alloc", "sd2_debug_expire_wait",
            "sd2_gemm_timing", "sd2_gemm_timing_read", "sd2_generate", "sd2_attention_flat_workspace_bytes",
            "sd2_attention_flat", "sd2_attention_prompt_workspace_bytes", "sd2_attention_prompt", "sd2_pages_append",
-           "sd2_pages_fork_workspace_bytes", "sd2_pages_fork", "sd2_pages_compact_workspace_bytes", "sd2_pages_compact"]
+           "sd2_pages_fork_workspace_bytes", "sd2_pages_fork", "sd2_pages_compact_workspace_bytes", "sd2_pages_compact",
+           "sd2_set_prompt_attention"]
 
 
 class LMConfig(ctypes.Structure):
@@ -116,6 +117,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sd2_gemm_timing_read.argtypes = [c_void_p, c_int32, POINTER(c_int32), POINTER(c_uint64), POINTER(c_double),
                                          POINTER(c_int32)]
     lib.sd2_debug_expire_wait.argtypes = [c_void_p, c_int64]
+    lib.sd2_set_prompt_attention.argtypes = [c_void_p, c_int32]
     lib.sd2_attention_prompt_workspace_bytes.argtypes = [c_int32] * 6
     lib.sd2_attention_prompt_workspace_bytes.restype = c_size_t
     lib.sd2_attention_prompt.argtypes = [c_void_p, c_int64, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int32,
@@ -302,6 +304,11 @@ class SD2Engine:
     def set_drafter_chain(self, enable: bool):
         """Drafter steps as one persistent kernel, or one kernel per projection (the default)."""
         self._call(self.lib.sd2_set_drafter_chain(self.ctx, 1 if enable else 0))
+
+    def set_prompt_attention(self, enable: bool):
+        """Prompts through the prompt attention kernel, or in small groups of rows through the decode kernel (the
+        default)."""
+        self._call(self.lib.sd2_set_prompt_attention(self.ctx, 1 if enable else 0))
 
     def set_fused_attention(self, enable: bool):
         """Batch-1 decode: attention inside the O projection, or its own kernel (the default)."""
