@@ -31,6 +31,7 @@
 #include <algorithm>
 #include <atomic>
 #include <string>
+#include <type_traits>
 
 namespace sd2 {
 void record_last_error(const std::string& m);  // engine.cu
@@ -782,19 +783,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
               if (!(seen & (1u << i))) x[c][i] = 0xFF800000u;   // -inf
           }
         }
-        auto tile_max = [&]() {
-          float top[4];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            top[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
-#pragma unroll
-            for (int i = 2; i < 32; i += 2)
-              top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])));
-          }
-          return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
-        };
-        // probabilities of columns 64 h .. 64 h + 63 as packed bf16, and their sum (of the unrounded ones)
-        auto half_exp = [&](int h, uint32_t (&p)[2][16]) {
+        // probabilities of columns 64 h .. 64 h + 63 as packed bf16, and their sum (of the unrounded ones);
+        // `with_max`: the maximum of the whole tile on the way (the two use different units)
+        float top[2] = {-INFINITY, -INFINITY};
+        auto half_exp = [&](int h, uint32_t (&p)[2][16], auto with_max) {
           const float base = m == -INFINITY ? 0.f : m;
           const uint64_t scale2 = pair(scale, scale), base2 = pair(-base, -base);
           uint64_t sum[2] = {0ull, 0ull};
@@ -807,6 +799,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
               unpair(fma2(pair(__uint_as_float(v[0]), __uint_as_float(v[1])), scale2, base2), e0, e1);
               e0 = ex2(e0);
               e1 = ex2(e1);
+              if (with_max) {
+                const uint32_t* y = x[2 * (1 - h) + c] + 2 * i;
+                top[0] = fmaxf(top[0], fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1])));
+                top[1] = fmaxf(top[1], fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
+              }
               sum[i & 1] = add2(sum[i & 1], pair(e0, e1));
               p[c][i] = pack_bf16(e0, e1);
             }
@@ -814,11 +811,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           unpair(add2(sum[0], sum[1]), s0, s1);
           return s0 + s1;
         };
-        // The first half is computed under the last maximum while this tile's is found (the two need different
-        // units); only if that has grown too much, or there is none yet, it is computed again.
+        // The first half is computed under the last maximum while this tile's is found; only if that has grown too
+        // much, or there is none yet, it is computed again.
         uint32_t p[2][16];
-        const float mx = tile_max();
-        float part = half_exp(0, p);
+        float part = half_exp(0, p, std::true_type());
+        const float mx = fmaxf(top[0], top[1]) * scale;
         const bool grown = mx > m + kGrowth || (m == -INFINITY && mx > m);
         if (Lay::kEarly && j > j0) {         // the last P has been read (and O has its product)
           if (!wait_warp(o_full + 8 * s, n_o++ & 1)) { ok = false; break; }
@@ -843,11 +840,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
               st32(to + c * 32, o);
             }
           }
-          part = half_exp(0, p);
+          part = half_exp(0, p, std::false_type());
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          if (h) part += half_exp(1, p);
+          if (h) part += half_exp(1, p, std::false_type());
           st16(tp + h * 32, p[0]);
           st16(tp + h * 32 + 16, p[1]);
           st_wait();                         // half of the tile's probabilities are there
@@ -1073,8 +1070,8 @@ sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t
     return fail(SD2_EINVAL, "bad attention shape (hd 64 or 128, H a multiple of Hkv, at most 128 heads per KV head)");
   if (n_blocks < 1 || bt_stride < 1 || bt_stride > (1 << 26) || layer < 0 || n_seq < 1 || max_kv < 1)
     return fail(SD2_EINVAL, "need n_blocks, bt_stride, n_seq, max_kv >= 1, bt_stride <= 2^26 and layer >= 0");
-  if (Hkv > 65535 || static_cast<int64_t>(n_blocks) * 2 * Hkv * kPage > INT32_MAX)
-    return fail(SD2_EINVAL, "a layer's K/V rows must be countable in 31 bits");
+  if (Hkv > 65535 || static_cast<int64_t>(n_blocks) * 2 * Hkv * kPage > INT32_MAX || static_cast<int64_t>(M) * H > INT32_MAX)
+    return fail(SD2_EINVAL, "a layer's K/V rows, and M * H, must be countable in 31 bits");
   if (ldq < static_cast<int64_t>(H) * hd || ldq % 8 || unaligned(d_q, 16) || unaligned(d_pool, 16) || unaligned(d_out, 16))
     return fail(SD2_EINVAL, "q rows, pool and out must be 16-byte aligned, ldq >= H * hd");
   if (M > 0 && workspace_bytes < sd2_attention_prompt_workspace_bytes(M, n_seq, H, Hkv, hd, max_kv))
