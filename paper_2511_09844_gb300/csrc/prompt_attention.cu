@@ -15,9 +15,10 @@
 //   warp 9          the MMAs: S = Q K^T from shared memory, O += P V with P in TMEM and V as the
 //                   [position][hd] tile that it is (MN-major); while one slot is in its softmax the
 //                   other's products run
-// TMEM: S0, S1 (P over them), O0, O1. O is rescaled in TMEM by the softmax threads, and only when a row's
-// maximum has grown by more than 2^8 since the last time: until then probabilities are taken relative to
-// the older maximum, which changes no rounding (bf16 and fp32 are relative) and cannot overflow.
+// TMEM: S0, S1, O0, O1 and P (over S for hd 128, where TMEM is full). Probabilities are taken relative to a
+// reference that starts at 0 (log2 units) and follows a row's maximum only when that has grown by more than 2^16
+// (or when its first scores lie 2^16 below): O is then rescaled in TMEM by the softmax threads. Any reference
+// that near gives the same relative rounding (bf16 and fp32 are relative) and neither over- nor underflows.
 //
 // Bound: the tensor cores for long prompts (4 hd flops per visible pair and head), HBM for few rows on a
 // long cache. Few rows leave SMs idle, so the positions are then cut over gridDim.z splits that a second
@@ -44,7 +45,8 @@ constexpr int kTile = 128;                 // positions per K/V tile, query vect
 constexpr int kThreads = 384;             // three warpgroups: 168 registers each at launch, then 216 / 216 / 72
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;    // 2 x 128 x 216 + 128 x 72 = 384 x 168
 constexpr int kMaxStages = 8;
-constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum that makes O be rescaled
+constexpr float kGrowth = 16.f;            // log2 of the growth of a maximum that makes O be rescaled
+constexpr float kDepth = 16.f;             // and how far below the reference a row's first scores may lie
 
 struct PromptArgs {
   CUtensorMap map_q, map_k, map_v;
@@ -420,7 +422,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         }
         if (w.jb >= w.je) continue;
         const int* row = a.table + static_cast<size_t>(w.seq) * a.bt_stride;
-        const int see = max(w.end[0], w.end[1]), n_pages = (see + kPage - 1) / kPage, step = 1 + w.solo;
+        const int see = max(w.end[0], w.end[1]), step = 1 + w.solo;
+        // K up to the last page seen; V, which the products take four pages at a time, up to a multiple of four
+        const int n_seen = (see + kPage - 1) / kPage;
+        const int n_pages = v_warp ? min((n_seen + 3) & ~3, (w.kv + kPage - 1) / kPage) : n_seen;
         const int page = v_warp ? lane : lane / kHalves, half = v_warp ? 0 : lane % kHalves;   // this lane's copy
         auto id_of = [&](int j) {
           const int i = j * (kTile / kPage) + page;
@@ -443,28 +448,29 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         auto load = [&](int j, int v, int page_id) {
           if (v == v_warp) {
             int np = min(kTile / kPage, n_pages - j * (kTile / kPage));
-            bool bad = page_id < 0 || page_id >= a.n_blocks;
+            const bool bad = page_id < 0 || page_id >= a.n_blocks;
             if (bad && page < np && a.err) atomicOr(a.err, static_cast<unsigned>(ERR_RANGE));
             if (!wait_warp(empty0 + 8 * st, ph ^ 1)) return false;
             const uint32_t dst = kv_smem + st * Lay::kSlotBytes;
             // a page that does not exist lies outside the map: zeros
             const int at = bad ? a.kv_rows : ((page_id * 2 + v) * a.Hkv + w.hk) * kPage;
             const int rows = w.kv - (j * kTile + (np - 1) * kPage);   // of the last page, that exist
-            if (v && rows < kPage) {
-              // Rows beyond the cached length hold anything, and a zero probability would not mask a NaN there: this
-              // page comes through registers, those rows as zeros.
-              --np;
-              const int src = __shfl_sync(0xffffffffu, at, np);
-              const bool none = __shfl_sync(0xffffffffu, static_cast<int>(bad), np);
+            if (v && ((np & 3) || rows < kPage)) {
+              // A zero probability would not mask a NaN: rows beyond the cached length, which hold anything, and pages
+              // beyond the last one are zeros here. A last page that is not whole comes through registers.
+              const int whole = rows < kPage ? np - 1 : np, end = (np + 3) & ~3;
+              const int src = __shfl_sync(0xffffffffu, at, np - 1);
+              const bool none = __shfl_sync(0xffffffffu, static_cast<int>(bad), np - 1);
 #pragma unroll 1
-              for (int i = lane; i < kPage * 8 * kHalves; i += 32) {
-                const int r = i / (8 * kHalves), c = i % (8 * kHalves);
+              for (int i = lane; i < (end - whole) * kPage * 8 * kHalves; i += 32) {
+                const int pg = whole + i / (kPage * 8 * kHalves), r = i / (8 * kHalves) % kPage, c = i % (8 * kHalves);
                 uint4 x = make_uint4(0, 0, 0, 0);
-                if (r < rows && !none)
+                if (pg < np && r < rows && !none)
                   x = *reinterpret_cast<const uint4*>(a.pool + (static_cast<size_t>(src) + r) * HD + c * 8);
-                *reinterpret_cast<uint4*>(smem + (dst - q_smem) + np * Lay::kPageBytes + (c / 8) * (kPage * 128) + r * 128 +
+                *reinterpret_cast<uint4*>(smem + (dst - q_smem) + pg * Lay::kPageBytes + (c / 8) * (kPage * 128) + r * 128 +
                                           ((c % 8) ^ (r & 7)) * 16) = x;
               }
+              np = whole;
               asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
               __syncwarp();
             }
@@ -502,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       if (elect_one()) {
         auto wait = [&](uint32_t bar, uint32_t parity) { return wait_spin(bar, parity, abort_flag, a.err); };
         constexpr uint32_t kSlot16 = Lay::kSlotBytes >> 4, kHalf16 = Lay::kHalf >> 4, kPage16 = Lay::kPageBytes >> 4;
-        const uint32_t idesc_s = idesc_bf16(kTile, 0), idesc_o = idesc_bf16(kTile, HD) | (1u << 16);   // B of P V is MN-major
+        const uint32_t idesc_s = idesc_bf16(kTile, kTile), idesc_o = idesc_bf16(kTile, HD) | (1u << 16);   // B of P V is MN-major
         const uint32_t q_desc = desc_k(q_smem), k_desc = desc_k(kv_smem), v_desc = desc_mn(kv_smem, kPage * 128);
         Work w;
         bool ok = true;
@@ -510,12 +516,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         uint32_t n_p[2] = {0, 0}, n_sc[2] = {0, 0};            // P and S tiles so far
         auto stage = [&](uint32_t i) { return i & (S - 1); };
         auto full = [&](uint32_t i) { return wait(full0 + 8 * stage(i), (i / S) & 1); };
-        auto issue_s = [&](int s, uint32_t a_desc, uint32_t st, uint32_t id) {
+        auto issue_s = [&](int s, uint32_t a_desc, uint32_t st) {
           const uint32_t b_desc = k_desc + st * kSlot16;
 #pragma unroll
           for (int kk = 0; kk < HD / 16; ++kk) {
             const uint32_t off = (kk / 4) * kHalf16 + (kk % 4) * 2;
-            mma_ss(tmem + s * kTile, a_desc + off, b_desc + off, id, kk > 0);
+            mma_ss(tmem + s * kTile, a_desc + off, b_desc + off, idesc_s, kk > 0);
           }
         };
         auto issue_o = [&](int s, uint32_t st, int part, uint32_t add) {
@@ -530,31 +536,23 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           const int step = 1 + w.solo;
           const int last[2] = {last_tile(w, 0), last_tile(w, 1)};
           auto active = [&](int s, int j) { return j < last[s] && (!w.solo || ((j - w.jb) & 1) == s); };
-          auto scores = [&](int s, int j, uint32_t st) {       // S_s = Q_s K_j^T over the pages that the slot sees
+          auto scores = [&](int s, uint32_t st) {              // S_s = Q_s K^T (columns of no page: anything, masked)
             if (Lay::kEarly) {                                 // the softmax has taken the last scores
               if (!wait(s_free + 8 * s, (n_sc[s] & 1) ^ 1)) { ok = false; return; }
               tc_fence_after();
             }
             ++n_sc[s];
-            const int n = min(kTile, ((s ? w.end[1] : w.end[0]) - j * kTile + kPage - 1) / kPage * kPage);
-            issue_s(s, q_desc + (w.solo ? 0 : s * kSlot16), st, idesc_s | (static_cast<uint32_t>(n >> 3) << 17));
+            issue_s(s, q_desc + (w.solo ? 0 : s * kSlot16), st);
             mma_commit(s_full + 8 * s);
           };
-          auto values = [&](int s, int j, uint32_t st) {       // O_s += P_s V_j, the halves of P as they come
-            const int steps = min(kTile / kPage, ((s ? w.end[1] : w.end[0]) - j * kTile + kPage - 1) / kPage);
+          auto values = [&](int s, int j, uint32_t st) {       // O_s += P_s V_j
             const uint32_t add = j >= w.jb + step ? 1u : 0u;
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
-              if (!ok || !wait(p_full + 16 * s + 8 * part, n_p[s] & 1)) { ok = false; continue; }
+            for (int part = 0; part < 2; ++part) {             // (the second half where the slot sees any of it)
+              if (ok && (!Lay::kEarly || part == 0)) ok = wait(p_full + 16 * s + 8 * part, n_p[s] & 1);
+              if (!ok) continue;
               tc_fence_after();
-              if (steps == kTile / kPage) {
-                issue_o(s, st, part, add);
-              } else {
-#pragma unroll 1
-                for (int kk = 4 * part; kk < min(steps, 4 * part + 4); ++kk)
-                  mma_ts(tmem + Lay::kO + s * HD, tmem + Lay::kP + s * Lay::kPStride + kk * 8,
-                         v_desc + st * kSlot16 + kk * kPage16, idesc_o, kk > 0 ? 1u : add);
-              }
+              if (part == 0 || (s ? w.end[1] : w.end[0]) - j * kTile > kTile / 2) issue_o(s, st, part, add);
             }
             ++n_p[s];
             // O has tile j (where the next scores follow P in its columns, their barrier says so too)
@@ -568,7 +566,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
             tc_fence_after();
 #pragma unroll
             for (int s = 0; s < 2; ++s)
-              if (ok && active(s, w.jb + i)) scores(s, w.jb + i, stage(u));
+              if (ok && active(s, w.jb + i)) scores(s, stage(u));
             mma_commit(empty0 + 8 * stage(u));
           }
           if (ok && w.jb + head == w.je) mma_commit(q_empty);  // every product that reads Q has been issued
@@ -576,7 +574,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           const int whole = w.solo ? 0 : min(w.je - 1, min(w.end[0], w.end[1]) / kTile - 1);
           for (int j = w.jb; j < w.je && ok; ++j) {
             if (j > w.jb && j < whole) {
-              constexpr uint32_t id = (1u << 4) | (1u << 7) | (1u << 10) | ((kTile >> 3) << 17) | ((kTile >> 4) << 24);
               uint32_t p0 = n_p[0] & 1, p1 = n_p[1] & 1, c0 = n_sc[0] & 1, c1 = n_sc[1] & 1;
               const int n = whole - j;
               int i = 0;
@@ -585,26 +582,22 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
                 if (Lay::kEarly) {
                   if (!full(u) || !wait(s_free, c0 ^ 1)) break;
                   tc_fence_after();
-                  issue_s(0, q_desc, st0, id);
+                  issue_s(0, q_desc, st0);
                   mma_commit(s_full);
                   if (!wait(s_free + 8, c1 ^ 1)) break;
                   tc_fence_after();
-                  issue_s(1, q_desc + kSlot16, st0, id);
+                  issue_s(1, q_desc + kSlot16, st0);
                   mma_commit(s_full + 8);
                   mma_commit(empty0 + 8 * st0);
                   if (!full(u + 1)) break;
                   if (!wait(p_full, p0)) break;
                   tc_fence_after();
                   issue_o(0, st1, 0, 1);
-                  if (!wait(p_full + 8, p0)) break;
-                  tc_fence_after();
                   issue_o(0, st1, 1, 1);
                   mma_commit(o_full);
                   if (!wait(p_full + 16, p1)) break;
                   tc_fence_after();
                   issue_o(1, st1, 0, 1);
-                  if (!wait(p_full + 24, p1)) break;
-                  tc_fence_after();
                   issue_o(1, st1, 1, 1);
                   mma_commit(o_full + 8);
                   mma_commit(empty0 + 8 * st1);
@@ -617,7 +610,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
                   issue_o(0, st0, 1, 1);
                   if (!full(u + 1)) break;
                   tc_fence_after();
-                  issue_s(0, q_desc, st1, id);
+                  issue_s(0, q_desc, st1);
                   mma_commit(s_full);
                   if (!wait(p_full + 16, p1)) break;
                   tc_fence_after();
@@ -626,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
                   tc_fence_after();
                   issue_o(1, st0, 1, 1);
                   mma_commit(empty0 + 8 * st0);
-                  issue_s(1, q_desc + kSlot16, st1, id);
+                  issue_s(1, q_desc + kSlot16, st1);
                   mma_commit(s_full + 8);
                   mma_commit(empty0 + 8 * st1);
                 }
@@ -652,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
                 take(k_st);
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
-                  if (ok && active(s, j) && j + step < last[s]) scores(s, j + step, k_st);
+                  if (ok && active(s, j) && j + step < last[s]) scores(s, k_st);
                 if (ok) mma_commit(empty0 + 8 * k_st);
               }
               if (ok) take(v_st);
@@ -670,7 +663,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
                 if (!ok || j + step >= last[s]) continue;
                 if (!have_k) take(k_st);
                 have_k = true;
-                if (ok) scores(s, j + step, k_st);
+                if (ok) scores(s, k_st);
               }
               if (ok) mma_commit(empty0 + 8 * v_st);
               if (ok && have_k) mma_commit(empty0 + 8 * k_st);
@@ -756,7 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         __syncwarp();
         if (lane == 0) done_reading();
       }
-      float m = -INFINITY, l = 0.f;
+      float m = 0.f, l = 0.f;
       for (int j = j0; j < je_s; j += step) {
         if (!wait_warp(s_full + 8 * s, n_s & 1)) { ok = false; break; }
         ++n_s;
@@ -787,8 +780,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         // `with_max`: the maximum of the whole tile on the way (the two use different units)
         float top[2] = {-INFINITY, -INFINITY};
         auto half_exp = [&](int h, uint32_t (&p)[2][16], auto with_max) {
-          const float base = m == -INFINITY ? 0.f : m;
-          const uint64_t scale2 = pair(scale, scale), base2 = pair(-base, -base);
+          const uint64_t scale2 = pair(scale, scale), base2 = pair(-m, -m);
           uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
           for (int c = 0; c < 2; ++c)
@@ -816,7 +808,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         uint32_t p[2][16];
         float part = half_exp(0, p, std::true_type());
         const float mx = fmaxf(top[0], top[1]) * scale;
-        const bool grown = mx > m + kGrowth || (m == -INFINITY && mx > m);
+        const bool grown = mx > m + kGrowth || (l == 0.f && mx < m - kDepth && mx > -INFINITY);
         if (Lay::kEarly && j > j0) {         // the last P has been read (and O has its product)
           if (!wait_warp(o_full + 8 * s, n_o++ & 1)) { ok = false; break; }
           tc_fence_after();
@@ -824,7 +816,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         if (__any_sync(0xffffffffu, grown)) {
           float f = 1.f;
           if (grown) {
-            f = ex2(m - mx);
+            f = l > 0.f ? ex2(m - mx) : 1.f;   // (nothing to rescale)
             m = mx;
             l *= f;
           }
@@ -847,10 +839,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           if (h) part += half_exp(1, p, std::false_type());
           st16(tp + h * 32, p[0]);
           st16(tp + h * 32 + 16, p[1]);
-          st_wait();                         // half of the tile's probabilities are there
+          if (Lay::kEarly && h == 0) continue;   // (the next scores do not wait for this product: P in one piece)
+          st_wait();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * h);
+          if (lane == 0) mbar_arrive(p_full + 16 * s + (Lay::kEarly ? 0 : 8 * h));
         }
         l += part;
       }
