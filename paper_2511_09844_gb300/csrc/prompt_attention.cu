@@ -159,6 +159,17 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ uint4 ld_shared(uint32_t saddr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(saddr));
+  return v;
+}
+__device__ __forceinline__ void st_shared(uint32_t saddr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(x), "r"(y), "r"(z), "r"(w));
+}
+__device__ __forceinline__ void st_global(unsigned char* p, const uint4& v) {
+  asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w));
+}
 // Two fp32 operations per instruction: a * b + c and a + b on packed pairs.
 __device__ __forceinline__ uint64_t pair(float lo, float hi) {
   uint64_t v;
@@ -725,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + lanes + s * kTile, to = tmem + lanes + Lay::kO + s * HD;
     const uint32_t tp = tmem + lanes + Lay::kP + s * Lay::kPStride;
-    unsigned char* panel = smem + (2 + S) * Lay::kSlotBytes + warp * 4096;
+    const uint32_t panel = q_smem + (2 + S) * Lay::kSlotBytes + warp * 4096;
     const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD));   // scores in log2
     uint32_t n_s = 0, n_o = 0;
     bool ok = true;
@@ -853,23 +864,22 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       const float inv = l > 0.f ? 1.f / l : 0.f;
       const size_t n_items = static_cast<size_t>(a.M) * a.H;
       const size_t part = (2 * static_cast<size_t>(split) + (solo ? s : 0)) * n_items + item;
-      // The results leave through a panel of 32 rows x 128 bytes, so that a store covers whole rows: straight from
-      // the lanes, each with a row of its own, every 16 bytes took a pass of the store path (7000 cycles a piece).
-      const unsigned rows_valid = __ballot_sync(0xffffffffu, valid);
+      // The results leave through a panel of 32 rows x 128 bytes (16-byte chunks rotated by the row), so that a store
+      // covers whole rows: straight from the lanes, each with a row of its own, every 16 bytes took a pass of the
+      // store path (7000 cycles a piece).
       const bool to_parts = a.n_splits > 1;
-      unsigned char* base = to_parts ? reinterpret_cast<unsigned char*>(a.part_o) : reinterpret_cast<unsigned char*>(a.out);
-      const size_t row_at = to_parts ? part * HD * 4 : item * HD * 2;
-      auto flush = [&](int byte0) {          // the panel to bytes byte0 .. byte0 + 127 of the rows
-        __syncwarp();
+      const unsigned rows_valid = __ballot_sync(0xffffffffu, valid);
+      const uint64_t row_ptr = to_parts ? reinterpret_cast<uint64_t>(a.part_o + part * HD)
+                                        : reinterpret_cast<uint64_t>(a.out + item * HD);
+      unsigned char* dst[8];                 // lane's 16 bytes of rows lane / 8, + 4, + 8 ..
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int row = i * 4 + lane / 8, c = lane % 8;
-          const uint4 v = *reinterpret_cast<const uint4*>(panel + row * 128 + ((c ^ (row & 7)) * 16));
-          const size_t at = __shfl_sync(0xffffffffu, static_cast<unsigned long long>(row_at), row);
-          if (rows_valid >> row & 1) *reinterpret_cast<uint4*>(base + at + byte0 + c * 16) = v;
-        }
-        __syncwarp();
-      };
+      for (int i = 0; i < 8; ++i) {
+        const int row = i * 4 + lane / 8;
+        const uint64_t at = __shfl_sync(0xffffffffu, static_cast<unsigned long long>(row_ptr), row);
+        dst[i] = rows_valid >> row & 1 ? reinterpret_cast<unsigned char*>(at) + lane % 8 * 16 : nullptr;
+      }
+      const uint32_t put = panel + lane * 128, put_x = (lane & 7) * 16;
+      const uint32_t get = panel + lane / 8 * 128 + ((lane % 8) ^ (lane / 8)) * 16;   // (row + 4 flips chunk bit 2)
 #pragma unroll 1
       for (int c = 0; c < HD / 32; ++c) {    // (not unrolled: the code of a rare path is fetched each time)
         uint32_t o[32];
@@ -877,17 +887,31 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         ld_wait(o);
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = l > 0.f ? __float_as_uint(__uint_as_float(o[i]) * inv) : 0u;
-        const int k0 = to_parts ? 0 : (c & 1) * 4;
-        if (!to_parts) {
+        if (to_parts) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] = pack_bf16(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1]));
+          for (int k = 0; k < 8; ++k) st_shared(put + ((k * 16) ^ put_x), o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              v[e] = pack_bf16(__uint_as_float(o[8 * k + 2 * e]), __uint_as_float(o[8 * k + 2 * e + 1]));
+            st_shared(put + (((c & 1) * 64 + k * 16) ^ put_x), v[0], v[1], v[2], v[3]);
+          }
+          if (!(c & 1)) continue;
         }
+        __syncwarp();
+        uint4 v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < 4 || to_parts)
-            *reinterpret_cast<uint4*>(panel + lane * 128 + (((k0 + k) ^ (lane & 7)) * 16)) =
-                make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-        if (to_parts || (c & 1)) flush(to_parts ? c * 128 : (c >> 1) * 128);
+        for (int i = 0; i < 8; ++i) v[i] = ld_shared((get + i * 512) ^ ((i & 1) * 64));
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (dst[i]) {
+            st_global(dst[i], v[i]);
+            dst[i] += 128;
+          }
+        __syncwarp();
       }
       if (valid) {
         const float l2 = l > 0.f ? m + log2f(l) : -INFINITY;
