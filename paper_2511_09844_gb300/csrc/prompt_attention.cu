@@ -16,9 +16,10 @@
 //                   [position][hd] tile that it is (MN-major); while one slot is in its softmax the
 //                   other's products run
 // TMEM: S0, S1, O0, O1 and P (over S for hd 128, where TMEM is full). Probabilities are taken relative to a
-// reference that starts at 0 (log2 units) and follows a row's maximum only when that has grown by more than 2^16
-// (or when its first scores lie 2^16 below): O is then rescaled in TMEM by the softmax threads. Any reference
-// that near gives the same relative rounding (bf16 and fp32 are relative) and neither over- nor underflows.
+// reference: a row's maximum over its first tile, then moved only when the maximum has grown by more than 2^8 (O is
+// then rescaled in TMEM by the softmax threads). A reference that near gives the same relative rounding (bf16 and
+// fp32 are relative) and cannot overflow; from the row's own maximum, the largest probability is exactly 1, so that
+// a row that sees one position gives its value unrounded.
 //
 // Bound: the tensor cores for long prompts (4 hd flops per visible pair and head), HBM for few rows on a
 // long cache. Few rows leave SMs idle, so the positions are then cut over gridDim.z splits that a second
@@ -45,8 +46,8 @@ constexpr int kTile = 128;                 // positions per K/V tile, query vect
 constexpr int kThreads = 384;             // three warpgroups: 168 registers each at launch, then 216 / 216 / 72
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;    // 2 x 128 x 216 + 128 x 72 = 384 x 168
 constexpr int kMaxStages = 8;
-constexpr float kGrowth = 16.f;            // log2 of the growth of a maximum that makes O be rescaled
-constexpr float kDepth = 16.f;             // and how far below the reference a row's first scores may lie
+constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum that makes O be rescaled
+constexpr float kNone = -1e30f;            // the reference before a row has seen anything
 
 struct PromptArgs {
   CUtensorMap map_q, map_k, map_v;
@@ -760,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         __syncwarp();
         if (lane == 0) done_reading();
       }
-      float m = 0.f, l = 0.f;
+      float m = kNone, l = 0.f;
       for (int j = j0; j < je_s; j += step) {
         if (!wait_warp(s_full + 8 * s, n_s & 1)) { ok = false; break; }
         ++n_s;
@@ -819,7 +820,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         uint32_t p[2][16];
         float part = half_exp(0, p, std::true_type());
         const float mx = fmaxf(top[0], top[1]) * scale;
-        const bool grown = mx > m + kGrowth || (l == 0.f && mx < m - kDepth && mx > -INFINITY);
+        const bool grown = mx > m + kGrowth;
         if (Lay::kEarly && j > j0) {         // the last P has been read (and O has its product)
           if (!wait_warp(o_full + 8 * s, n_o++ & 1)) { ok = false; break; }
           tc_fence_after();
