@@ -828,7 +828,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         if (__any_sync(0xffffffffu, grown)) {
           float f = 1.f;
           if (grown) {
-            f = l > 0.f ? ex2(m - mx) : 1.f;   // (nothing to rescale)
+            f = ex2(m - mx);                 // (0 where nothing had been seen)
             m = mx;
             l *= f;
           }
@@ -862,7 +862,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       if (je_s > j0 && ok) ok = wait_warp(o_full + 8 * s, n_o++ & 1);
       if (!ok) break;
       tc_fence_after();
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const bool none = l == 0.f;            // nothing seen (a NaN is passed on)
+      const float inv = 1.f / l;
       const size_t n_items = static_cast<size_t>(a.M) * a.H;
       const size_t part = (2 * static_cast<size_t>(split) + (solo ? s : 0)) * n_items + item;
       // The results leave through a panel of 32 rows x 128 bytes (16-byte chunks rotated by the row), so that a store
@@ -887,7 +888,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         ld32(to + c * 32, o);
         ld_wait(o);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = l > 0.f ? __float_as_uint(__uint_as_float(o[i]) * inv) : 0u;
+        for (int i = 0; i < 32; ++i) o[i] = none ? 0u : __float_as_uint(__uint_as_float(o[i]) * inv);
         if (to_parts) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) st_shared(put + ((k * 16) ^ put_x), o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
@@ -915,7 +916,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         __syncwarp();
       }
       if (valid) {
-        const float l2 = l > 0.f ? m + log2f(l) : -INFINITY;
+        const float l2 = none ? -INFINITY : m + log2f(l);
         if (a.n_splits > 1) {
           a.part_lse[part] = l2;
           if (!solo) a.part_lse[part + n_items] = -INFINITY;   // no second half
@@ -980,12 +981,12 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant_
     }
   }
   if (item >= n || static_cast<int>(item / a.H) >= rows) return;
-  const float inv = total > 0.f ? 1.f / total : 0.f;
+  const float inv = total == 0.f ? 0.f : 1.f / total;   // (a NaN is passed on)
   struct alignas(2 * kPer) Out { uint32_t v[kPer / 2]; } out;
 #pragma unroll
   for (int i = 0; i < kPer; i += 2) out.v[i / 2] = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
   *reinterpret_cast<Out*>(a.out + item * HD + lane * kPer) = out;
-  if (a.lse && lane == 0) a.lse[item] = total > 0.f ? (mx + log2f(total)) * 0.6931471805599453f : -INFINITY;
+  if (a.lse && lane == 0) a.lse[item] = total == 0.f ? -INFINITY : (mx + log2f(total)) * 0.6931471805599453f;
 }
 
 // The grid: query tiles (an upper bound: the sequences' lengths are on the device), and splits of the

@@ -313,3 +313,51 @@ def test_fork_then_compact_keeps_every_position():
         for j, x in enumerate(before[b]):
             assert torch.equal(x, _bits(pool[:, c.table[b, j // 16], :, :, j % 16]))
     assert int(c.table.max()) < int(c.n_live)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_fork_chains_beyond_one_block(seed):
+    """The same rules where the plan runs over several blocks: a pool larger than one block counts, or a batch."""
+    r = random.Random(100 + seed)
+    n_blocks, stride, n = (13000, 40, 5) if seed % 2 else (900, 33, 2100)
+    pool = _pool(1, n_blocks, 1, 8, seed)
+    lens = [r.randrange(0, 300) for _ in range(6)]
+    table = _fresh(lens, stride, n_blocks, seed)
+    pinned = [1 if r.random() < 0.1 else 0 for _ in range(n_blocks)]
+    for _ in range(2):
+        parent = [r.randrange(-1, len(table)) for _ in range(n)]
+        keep = [r.randrange(0, 16 * stride) if r.random() < 0.5 else lens[p] if p >= 0 else 0 for p in parent]
+        f = _fork_check(pool, table, lens, parent, keep, [r.choice((0, 0, 0, 1, 20)) for _ in parent], pinned)
+        table, lens = f.table.tolist(), f.length.tolist()
+
+
+def test_page_operators_in_a_captured_graph():
+    """Fork and compaction replayed on other tables give those tables' results."""
+    lens = [50, 20]
+    pool = _pool(1, 32, 1, 64, 5)
+    a, b = _fresh(lens, 5, 32, 1), _fresh(lens, 5, 32, 2)
+    live, n, parent = _i(a), _i(lens), _i([0, 1, 0])
+    side = torch.cuda.Stream()
+
+    def both():
+        f = sd2.pages_fork(pool, live, n, parent, grow=None)
+        return f, sd2.pages_compact(pool, f.table, f.pages, f.ref)
+    with torch.cuda.stream(side):
+        both()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            f, c = both()
+    for table in (a, b):
+        fresh = _pool(1, 32, 1, 64, 6)
+        pool.copy_(fresh)
+        live.copy_(_i(table))
+        want = _fork_reference(fresh, table, lens, [0, 1, 0], None, None, None)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert f.table.tolist() == want[0] and f.length.tolist() == want[1] and f.ref.tolist() == want[3]
+        for s in range(3):
+            for j in range(want[1][s]):
+                got = pool[0, c.table[s, j // 16], :, :, j % 16]
+                assert torch.equal(_bits(got), _bits(want[4][0, want[0][s][j // 16], :, :, j % 16]))

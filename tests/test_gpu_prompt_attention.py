@@ -286,3 +286,106 @@ def test_refusals_of_device_tensors():
         with pytest.raises(sd2.SD2Error, match="EINVAL"):
             sd2.attention_prompt(**dict(ok, **bad))
     assert sd2.attention_prompt(**dict(ok, q=d["q"][:0], cu_rows=d["cu"] * 0)).shape == (0, 256)
+
+
+@pytest.mark.parametrize("n", [33, 70])
+@pytest.mark.parametrize("H,Hkv,hd", [(8, 2, 128), (14, 2, 64)])
+def test_many_sequences(n, H, Hkv, hd):
+    """More sequences than one warp holds at a time, empty ones and prefixes among them."""
+    g = torch.Generator().manual_seed(n)
+    rows = [int(x) for x in torch.randint(0, 90, (n,), generator=g)]
+    rows[3] = rows[n - 1] = 0
+    prefix = [int(x) if i % 3 else 0 for i, x in enumerate(torch.randint(0, 200, (n,), generator=g))]
+    c = _case(rows, [a + b for a, b in zip(rows, prefix)], H, Hkv, hd, seed=n)
+    out, lse, err = _run(c)
+    assert err == 0
+    _check(c, out, lse)
+
+
+def test_many_sequences_of_one_row_each():
+    """A decode batch through the prompt kernel: 40 sequences, split."""
+    kv = [1 + 37 * i for i in range(40)]
+    c = _case([1] * 40, kv, 2, 1, 128, seed=41)
+    out, lse, err = _run(c)
+    assert err == 0
+    _check(c, out, lse)
+
+
+def test_two_streams_at_once():
+    """Calls that overlap on the GPU, each with its own workspace and error word, keep their own results."""
+    cases = [_case([300, 45], [300, 700], 8, 2, 128, seed=51), _case([2, 7], [3000, 2500], 14, 2, 64, seed=52)]
+    want = [_run(c)[:2] for c in cases]
+    dev = [{k: v.cuda() for k, v in c.items() if isinstance(v, torch.Tensor)} for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, (c, d, st) in enumerate(zip(cases, dev, streams)):
+            got[i].append(sd2.attention_prompt(d["q"], d["pool"], d["table"], c["layer"], d["cu"], d["kv_len"],
+                                               max_kv=max(c["kv"]), return_lse=True, stream=st))
+    torch.cuda.synchronize()
+    for i, (out, lse) in enumerate(want):
+        for o, l in got[i]:
+            assert torch.equal(o.cpu(), out) and torch.equal(l.cpu(), lse)
+
+
+def test_captured_call_follows_the_device_lengths():
+    """A captured call reads offsets and lengths when it is replayed: other lengths, other results, no recapture."""
+    a = _case([100, 20], [100, 420], 8, 2, 128, seed=61)
+    b = _case([20, 100], [320, 100], 8, 2, 128, seed=61, slack=9)     # another division of the same 120 rows
+    want = [_definition(a), _definition(b)]
+    width = max(a["table"].shape[1], b["table"].shape[1])
+    n_blocks = max(a["pool"].shape[1], b["pool"].shape[1])
+    dev = {}
+    for name, c in (("a", a), ("b", b)):
+        t = torch.zeros(2, width, dtype=torch.int32)
+        t[:, :c["table"].shape[1]] = c["table"]
+        p = torch.zeros(2, n_blocks, *c["pool"].shape[2:], dtype=torch.bfloat16)
+        p[:, :c["pool"].shape[1]] = c["pool"]
+        dev[name] = [x.cuda() for x in (c["q"], p, t, c["cu"], c["kv_len"])]
+    live = [x.clone() for x in dev["a"]]
+    call = lambda: sd2.attention_prompt(live[0], live[1], live[2], 1, live[3], live[4], max_kv=420, return_lse=True)  # noqa: E731
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out, lse = call()
+    for name, c, w in (("a", a, want[0]), ("b", b, want[1]), ("a", a, want[0])):
+        for x, y in zip(live, dev[name]):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(c, out.cpu(), lse.cpu(), w)
+
+
+def test_rows_beside_other_sequences_nan():
+    """A sequence whose queries are NaN, or whose cache is, spoils its own rows only."""
+    c = _case([40, 30, 50], [40, 300, 50], 8, 2, 128, seed=71)
+    want = _definition(c)
+    c["q"][45:50] = float("nan")
+    ids = c["table"][2, :4].long()
+    c["pool"][c["layer"], ids] = float("nan")
+    out, lse, err = _run(c)
+    assert err == 0
+    o, l, mag = want
+    keep = [i for i in range(70) if not 45 <= i < 50]
+    assert ((out[keep].double() - o[keep]).abs() - _bound(o[keep], mag[keep])).max().item() <= 1e-6
+    assert torch.isnan(out[45:50].float()).all() and torch.isnan(out[70:].float()).all()
+
+
+def test_nan_through_split_caches():
+    """The same where the positions are split and joined: a NaN anywhere in what a row sees reaches that row."""
+    c = _case([1, 2], [3000, 2600], 8, 2, 128, seed=72)
+    want = _definition(c)
+    c["pool"][c["layer"], c["table"][1, 100].long(), 0, 1, 3] = float("nan")     # position 1603, KV head 1
+    out, lse, err = _run(c)
+    o, l, mag = want
+    assert err == 0
+    clean = torch.ones(3, 8, 128, dtype=torch.bool)
+    clean[1:, 4:] = False                                                        # heads 4 .. 7 of sequence 1
+    off = ((out.double() - o).abs() - _bound(o, mag)).view(3, 8, 128)
+    assert off[clean].max().item() <= 1e-6
+    assert torch.isnan(out.float().view(3, 8, 128)[~clean]).all() and torch.isnan(lse[1:, 4:]).all()
+    assert torch.isfinite(lse[0]).all() and torch.isfinite(lse[1:, :4]).all()
