@@ -267,13 +267,19 @@ __device__ __forceinline__ int warp_scan(int v) {
   return v;
 }
 
-// Finds tile `tile` of the grid (one warp). Up to 32 sequences: tiles are numbered by the K/V tiles that they
-// walk, the longest first, so that the short ones fill the end of the grid. More sequences: through the
-// sequences, each from its last (longest) tile.
-__device__ bool find_work(const PromptArgs& a, const Seqs& first, int tile, int hk, int split, Work& w) {
+// Finds the piece of block (x, split) of the grid, tile x / Hkv of KV head x % Hkv (one warp). Up to 32 sequences:
+// tiles are numbered by the K/V tiles that they walk, the longest first, so that the short ones fill the end of the
+// grid. More sequences: through the sequences, each from its last (longest) tile; the search goes on where the last
+// one ended (a block's pieces come in order).
+struct Cursor {
+  Seqs f;                                  // sequences s0 .. s0 + 31, one per lane
+  int s0, before;                          // and the tiles of those before them
+};
+__device__ bool find_work(const PromptArgs& a, Cursor& at, int x, int split, Work& w) {
   const int lane = threadIdx.x & 31, per = 2 * a.T;
-  Seqs f = first;
-  int s0 = 0, src = -1, t = 0;
+  const int tile = x / a.Hkv, hk = x - tile * a.Hkv;
+  Seqs& f = at.f;
+  int src = -1, t = 0;
   if (a.n_seq <= 32) {
     if (tile >= __reduce_add_sync(0xffffffffu, f.n)) return false;
     // the largest e with more than `tile` tiles that walk at least e K/V tiles
@@ -293,22 +299,27 @@ __device__ bool find_work(const PromptArgs& a, const Seqs& first, int tile, int 
       t = __shfl_sync(0xffffffffu, f.n - 1 - more - (rank - (sum - (at_least - more))), src);
     }
   } else {
-    for (int before = 0; s0 < a.n_seq; s0 += 32) {
-      if (s0) f.load(a, s0 + lane);
-      const int sum = before + warp_scan(f.n);
+    if (tile < at.before) {
+      at.s0 = at.before = 0;
+      f.load(a, lane);
+    }
+    while (true) {
+      const int sum = at.before + warp_scan(f.n);
       const unsigned hit = __ballot_sync(0xffffffffu, sum > tile);
       if (hit) {
         src = __ffs(hit) - 1;
         t = __shfl_sync(0xffffffffu, sum - 1 - tile, src);
         break;
       }
-      before = __shfl_sync(0xffffffffu, sum, 31);
+      if (at.s0 + 32 >= a.n_seq) return false;
+      at.before = __shfl_sync(0xffffffffu, sum, 31);
+      at.s0 += 32;
+      f.load(a, at.s0 + lane);
     }
-    if (src < 0) return false;
   }
   const int lo = __shfl_sync(0xffffffffu, f.lo, src), rows = __shfl_sync(0xffffffffu, f.rows, src);
   const int len = __shfl_sync(0xffffffffu, f.len, src);
-  w.seq = s0 + src;
+  w.seq = at.s0 + src;
   w.hk = hk;
   w.split = split;
   w.row0 = lo + t * per;
@@ -368,11 +379,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
   volatile int* abort_flag = flags;
   if (a.n_splits > 1) pdl_trigger();       // the join may be set up (it waits for this grid to complete)
   Work first{};
-  Seqs finder{};
+  Cursor cursor{};
   bool found = false;
   if (warp == 10) {
-    finder.load(a, lane);
-    found = find_work(a, finder, blockIdx.y, blockIdx.x, blockIdx.z, first);
+    cursor.f.load(a, lane);
+    found = find_work(a, cursor, blockIdx.x, blockIdx.z, first);
     if (lane == 0) {
       works[0] = first;
       flags[2] = found;
@@ -727,7 +738,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         const bool more = read_block(smem_u32(&answer), x, y, z);
         __syncwarp();
         if (!more) break;
-        found = find_work(a, finder, y, x, z, first);
+        found = find_work(a, cursor, x, z, first);
       }
       if (ok) {
         const uint32_t i = n & 1;
@@ -1033,7 +1044,7 @@ cudaError_t launch(const PromptArgs& a, int tiles, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     if (dev <= 63) set.fetch_or(1ull << dev);
   }
-  prompt_attention_kernel<HD><<<dim3(a.Hkv, tiles, a.n_splits), kThreads, smem, st>>>(a);
+  prompt_attention_kernel<HD><<<dim3(a.Hkv * tiles, 1, a.n_splits), kThreads, smem, st>>>(a);
   if ((e = cudaGetLastError()) != cudaSuccess || a.n_splits == 1) return e;
   const long long items = static_cast<long long>(a.M) * a.H;
   if (a.n_splits <= 4) return launch_pdl(prompt_join_kernel<HD, 1>, dim3(static_cast<unsigned>((items + 3) / 4)), dim3(128), 0, st, a);
@@ -1099,7 +1110,7 @@ sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t
     return fail(SD2_EINVAL, "bad attention shape (hd 64 or 128, H a multiple of Hkv, at most 128 heads per KV head)");
   if (n_blocks < 1 || bt_stride < 1 || bt_stride > (1 << 26) || layer < 0 || n_seq < 1 || max_kv < 1)
     return fail(SD2_EINVAL, "need n_blocks, bt_stride, n_seq, max_kv >= 1, bt_stride <= 2^26 and layer >= 0");
-  if (Hkv > 65535 || static_cast<int64_t>(n_blocks) * 2 * Hkv * kPage > INT32_MAX || static_cast<int64_t>(M) * H > INT32_MAX)
+  if (static_cast<int64_t>(n_blocks) * 2 * Hkv * kPage > INT32_MAX || static_cast<int64_t>(M) * H > INT32_MAX)
     return fail(SD2_EINVAL, "a layer's K/V rows, and M * H, must be countable in 31 bits");
   if (ldq < static_cast<int64_t>(H) * hd || ldq % 8 || unaligned(d_q, 16) || unaligned(d_pool, 16) || unaligned(d_out, 16))
     return fail(SD2_EINVAL, "q rows, pool and out must be 16-byte aligned, ldq >= H * hd");

@@ -389,3 +389,28 @@ def test_nan_through_split_caches():
     assert off[clean].max().item() <= 1e-6
     assert torch.isnan(out.float().view(3, 8, 128)[~clean]).all() and torch.isnan(lse[1:, 4:]).all()
     assert torch.isfinite(lse[0]).all() and torch.isfinite(lse[1:, :4]).all()
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(128, 1, 64), (2, 2, 64)])
+def test_thousands_of_sequences(H, Hkv, hd):
+    """More tiles than a grid's second dimension holds, and a search over thousands of sequences (spot checks:
+    all share one page table row's pages, so the definition is that of one sequence)."""
+    n = 33000
+    g = torch.Generator().manual_seed(81)
+    pool = torch.randn(1, 2, 2, Hkv, 16, hd, generator=g).to(torch.bfloat16)
+    rows = torch.randint(1, 5, (n,), generator=g)
+    rows[7] = 0
+    cu = torch.cat([torch.zeros(1, dtype=torch.long), rows.cumsum(0)])
+    kv = rows + torch.randint(0, 20, (n,), generator=g)
+    M = int(cu[-1])
+    q = torch.randn(M, H, hd, generator=g).to(torch.bfloat16)
+    table = torch.tensor([[1, 0]], dtype=torch.int32).expand(n, 2).contiguous()
+    out, lse = sd2.attention_prompt(q.cuda(), pool.cuda(), table.cuda(), 0, cu.int().cuda(), kv.int().cuda(), max_kv=24,
+                                    return_lse=True)
+    out, lse = out.cpu(), lse.cpu()
+    for s in [0, 1, 6, 8, 31, 32, 33, 63, 64, 1000, 16500, n - 33, n - 2, n - 1]:
+        a, b, L = int(cu[s]), int(cu[s + 1]), int(kv[s])
+        c = dict(q=q[a:b], pool=pool, table=table[:1], layer=0, cu=torch.tensor([0, b - a]), rows=[b - a], kv=[L], H=H,
+                 Hkv=Hkv, hd=hd)
+        _check(c, out[a:b], lse[a:b])
+    assert torch.isfinite(lse).all()
