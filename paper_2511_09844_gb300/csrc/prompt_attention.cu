@@ -27,8 +27,8 @@
 // Bound: the tensor cores for long prompts with heads of 128 (4 hd flops per visible pair and head), the
 // softmax's instructions with heads of 64 (about 550 per warp and 32 x 128 scores, issued every second cycle),
 // HBM for few rows on a long cache, latency for short prompts. Few rows leave SMs idle, so the positions are
-// then cut over gridDim.z splits that a second kernel joins; their blocks put both slots on the same queries
-// and give them alternate K/V tiles.
+// then cut over gridDim.z splits that a second kernel joins. A piece with queries for one slot only puts both
+// slots on them, with alternate K/V tiles, and joins the two at its end (slot 0's threads read slot 1's columns).
 //
 // Measured (GB300, 1913 TFLOP/s bf16 and 6.77 TB/s copy): one prompt of 16384, 32/8 heads of 128, 1.15-1.25 ms,
 // 1.76-1.9 PFLOP/s; four chunks of 411-777 rows on 3K-16K positions, 40/8 heads of 128, 457 us, 1.73 PFLOP/s; one
@@ -57,6 +57,9 @@ constexpr int kThreads = 384;             // three warpgroups: 168 registers eac
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;    // 2 x 128 x 216 + 128 x 72 = 384 x 168
 constexpr int kMaxStages = 8;
 constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum that makes O be rescaled
+// K/V tiles from which on two slots share the work of one and join (256 sequences of 9 rows on 500 positions, 32/8 heads
+// of 64: 96 us from 4 on, 109 from 8 on; one row on 1000 positions, 32/8 heads of 128: 11.9 us from 2 on, 11.4 from 4 on)
+constexpr int kSoloTiles = 4;
 constexpr float kNone = -1e30f;            // the reference before a row has seen anything
 
 struct PromptArgs {
@@ -68,7 +71,7 @@ struct PromptArgs {
   const bf16* pool;                        // the layer's pages
   bf16* out;
   float* lse;
-  float *part_o, *part_lse;                // [2 n_splits][M * H][hd] and [2 n_splits][M * H] (log2)
+  float *part_o, *part_lse;                // [n_splits][M * H][hd] and [n_splits][M * H] (log2)
   unsigned* err;
 };
 
@@ -84,14 +87,14 @@ struct Layout {
   static constexpr int kO = 2 * kTile, kP = HD == 128 ? 0 : 2 * kTile + 2 * HD, kPStride = HD == 128 ? kTile : kTile / 2;
   // P apart from S: the next scores are computed while the softmax of the current ones runs
   static constexpr bool kEarly = HD != 128;
-  static constexpr int kSmem = kBytes + 1024 + 256;     // + alignment + barriers
+  static constexpr int kSmem = kBytes + 1024;           // + alignment
 };
 
 // One piece of work: two query tiles (slots) of a sequence and KV head against some of its K/V tiles.
 struct Work {
   int seq, hk, split;                      // seq < 0: no more work
   int row0, pos0, kv;                      // first packed row and its position, positions that exist
-  int solo;                                // both slots hold slot 0's tokens and take K/V tiles in turn
+  int solo;                                // both slots hold the same tokens, take K/V tiles in turn and are joined
   int tokens[2];                           // of each slot
   int end[2];                              // positions the slot sees: [0, end)
   int jb, je;                              // K/V tiles of this split
@@ -325,16 +328,19 @@ __device__ bool find_work(const PromptArgs& a, Cursor& at, int x, int split, Wor
   w.row0 = lo + t * per;
   w.pos0 = len - rows + t * per;
   w.kv = min(max(len, 0), a.bt_stride * kPage);
-  w.solo = a.n_splits > 1 && rows - t * per <= a.T;
+  // tokens for one slot only: both take them, where there are enough K/V tiles
+  const bool few = rows - t * per <= a.T;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int from = w.solo ? 0 : i * a.T;
+    const int from = few ? 0 : i * a.T;
     w.tokens[i] = min(max(rows - t * per - from, 0), a.T);
     w.end[i] = w.tokens[i] ? min(max(w.pos0 + from + w.tokens[i], 0), w.kv) : 0;
   }
   const long long nt = (max(w.end[0], w.end[1]) + kTile - 1) / kTile;
   w.jb = static_cast<int>(nt * split / a.n_splits);
   w.je = static_cast<int>(nt * (split + 1) / a.n_splits);
+  w.solo = few && w.je - w.jb >= kSoloTiles;
+  if (few && !w.solo) w.tokens[1] = w.end[1] = 0;
   return true;
 }
 
@@ -369,12 +375,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   __shared__ Work works[2];
   __shared__ __align__(16) uint4 answer;
+  __shared__ float twin[2][kTile];         // slot 1's references and sums, for slot 0 (solo work)
   __shared__ int flags[3];                 // [0] abort, [1] TMEM base, [2] the block has work of its own
-  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 20];
+  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 22];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * S, q_full = empty0 + 8 * S, q_empty = q_full + 8,
                  s_full = q_empty + 8, s_free = s_full + 16, o_full = s_free + 16, p_full = o_full + 16, drain = p_full + 32,
-                 w_full = drain + 8, w_empty = w_full + 16, w_taken = w_empty + 16, given = w_taken + 8;
+                 w_full = drain + 8, w_empty = w_full + 16, w_taken = w_empty + 16, given = w_taken + 8,
+                 t_ready = given + 8, t_done = t_ready + 8;
   const uint32_t q_smem = smem_u32(smem), kv_smem = q_smem + 2 * Lay::kSlotBytes;
   volatile int* abort_flag = flags;
   if (a.n_splits > 1) pdl_trigger();       // the join may be set up (it waits for this grid to complete)
@@ -414,6 +422,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
     mbar_init(drain, 1);
     mbar_init(w_taken, 1);
     mbar_init(given, 1);
+    mbar_init(t_ready, 4);
+    mbar_init(t_done, 4);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tc_fence_before();
@@ -760,7 +770,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
     const uint32_t tp = tmem + lanes + Lay::kP + s * Lay::kPStride;
     const uint32_t panel = q_smem + (2 + S) * Lay::kSlotBytes + warp * 4096;
     const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD));   // scores in log2
-    uint32_t n_s = 0, n_o = 0;
+    uint32_t n_s = 0, n_o = 0, n_t = 0;
     bool ok = true;
     while (ok) {
       int j0, je_s, step, see_r, split, solo;
@@ -883,10 +893,42 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       if (je_s > j0 && ok) ok = wait_warp(o_full + 8 * s, n_o++ & 1);
       if (!ok) break;
       tc_fence_after();
+      if (solo) {                            // slot 0 adds slot 1's results, read from TMEM, to its own
+        if (s == 1) {
+          twin[0][r] = m;
+          twin[1][r] = l;
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(t_ready);
+          if (!(ok = wait_warp(t_done, n_t++ & 1))) break;
+          continue;
+        }
+        if (!(ok = wait_warp(t_ready, n_t++ & 1))) break;
+        tc_fence_after();
+        const float m1 = twin[0][r], l1 = twin[1][r], top = fmaxf(m, m1), f0 = ex2(m - top), f1 = ex2(m1 - top);
+#pragma unroll 1
+        for (int c = 0; c < HD / 32; ++c) {
+          uint32_t o[32], o1[32];
+          ld32(to + c * 32, o);
+          ld32(to + HD + c * 32, o1);
+          ld_wait(o);
+          ld_tie(o1);
+#pragma unroll
+          for (int i = 0; i < 32; ++i)       // (where a slot saw nothing its columns may hold anything)
+            o[i] = __float_as_uint((l == 0.f ? 0.f : __uint_as_float(o[i]) * f0) + (l1 == 0.f ? 0.f : __uint_as_float(o1[i]) * f1));
+          st32(to + c * 32, o);
+        }
+        st_wait();
+        l = l * f0 + l1 * f1;
+        m = top;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(t_done);  // slot 1's columns may be written again
+      }
       const bool none = l == 0.f;            // nothing seen (a NaN is passed on)
       const float inv = 1.f / l;
       const size_t n_items = static_cast<size_t>(a.M) * a.H;
-      const size_t part = (2 * static_cast<size_t>(split) + (solo ? s : 0)) * n_items + item;
+      const size_t part = static_cast<size_t>(split) * n_items + item;
       // The results leave through a panel of 32 rows x 128 bytes (16-byte chunks rotated by the row), so that a store
       // covers whole rows: straight from the lanes, each with a row of its own, every 16 bytes took a pass of the
       // store path (7000 cycles a piece).
@@ -938,12 +980,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       }
       if (valid) {
         const float l2 = none ? -INFINITY : m + log2f(l);
-        if (a.n_splits > 1) {
-          a.part_lse[part] = l2;
-          if (!solo) a.part_lse[part + n_items] = -INFINITY;   // no second half
-        } else if (a.lse) {
-          a.lse[item] = l2 * 0.6931471805599453f;
-        }
+        if (to_parts) a.part_lse[part] = l2;
+        else if (a.lse) a.lse[item] = l2 * 0.6931471805599453f;
       }
     }
   }
@@ -963,7 +1001,7 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant_
   __shared__ float acc_s[4][HD + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % W;
   const size_t item = static_cast<size_t>(blockIdx.x) * (4 / W) + warp / W, n = static_cast<size_t>(a.M) * a.H;
-  const int parts = item < n ? 2 * a.n_splits : 0;
+  const int parts = item < n ? a.n_splits : 0;
   const int rows = a.cu[a.n_seq];
   float mx = -INFINITY;
   for (int z = lane; z < parts; z += 32) mx = fmaxf(mx, a.part_lse[z * n + item]);
@@ -1047,7 +1085,7 @@ cudaError_t launch(const PromptArgs& a, int tiles, cudaStream_t st) {
   prompt_attention_kernel<HD><<<dim3(a.Hkv * tiles, 1, a.n_splits), kThreads, smem, st>>>(a);
   if ((e = cudaGetLastError()) != cudaSuccess || a.n_splits == 1) return e;
   const long long items = static_cast<long long>(a.M) * a.H;
-  if (a.n_splits <= 4) return launch_pdl(prompt_join_kernel<HD, 1>, dim3(static_cast<unsigned>((items + 3) / 4)), dim3(128), 0, st, a);
+  if (a.n_splits <= 8) return launch_pdl(prompt_join_kernel<HD, 1>, dim3(static_cast<unsigned>((items + 3) / 4)), dim3(128), 0, st, a);
   return launch_pdl(prompt_join_kernel<HD, 4>, dim3(static_cast<unsigned>(items)), dim3(128), 0, st, a);
 }
 
@@ -1055,7 +1093,7 @@ cudaError_t launch(const PromptArgs& a, int tiles, cudaStream_t st) {
 
 size_t prompt_attention_work_bytes(int M, int n_seq, int H, int Hkv, int hd, int max_kv) {
   const int splits = shape_of(M, n_seq, H, Hkv, hd, max_kv).splits;
-  return splits > 1 ? static_cast<size_t>(2 * splits) * M * H * (hd + 1) * 4 : 0;
+  return splits > 1 ? static_cast<size_t>(splits) * M * H * (hd + 1) * 4 : 0;
 }
 
 cudaError_t prompt_attention(const PromptAttnArgs& p, cudaStream_t st) {
@@ -1067,7 +1105,7 @@ cudaError_t prompt_attention(const PromptAttnArgs& p, cudaStream_t st) {
   a.n_seq = p.n_seq; a.n_splits = p.work ? s.splits : 1; a.kv_rows = p.kv.n_blocks * 2 * Hkv * kPage;
   a.table = p.kv.table; a.cu = p.cu; a.kv_len = p.kv_len; a.out = static_cast<bf16*>(p.out); a.lse = p.lse; a.err = p.err;
   a.part_o = static_cast<float*>(p.work);
-  a.part_lse = a.part_o + static_cast<size_t>(2 * a.n_splits) * p.M * p.H * hd;
+  a.part_lse = a.part_o + static_cast<size_t>(a.n_splits) * p.M * p.H * hd;
   a.pool = static_cast<const bf16*>(p.kv.pool) + static_cast<size_t>(p.layer) * p.kv.n_blocks * 2 * Hkv * kPage * hd;
   // Q: [row][head][hd], boxes of T rows x G heads x 64; K: [page row][hd], a page x 64; V: a page x all of hd,
   // one 64-column half behind the other

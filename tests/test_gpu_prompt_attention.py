@@ -414,3 +414,15 @@ def test_thousands_of_sequences(H, Hkv, hd):
                  Hkv=Hkv, hd=hd)
         _check(c, out[a:b], lse[a:b])
     assert torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(4, 4, 64), (8, 2, 128), (14, 2, 64)])
+@pytest.mark.parametrize("claim", [1, 1 << 20])
+def test_pieces_for_one_query_tile(H, Hkv, hd, claim):
+    """Rows that fill no more than one query tile: both take turns over the cache and are joined, with one to many
+    K/V tiles for them, rows that see only the first of them, or none."""
+    rows, kv = [1, 3, 20, 9, 7, 12, 5], [128, 129, 300, 1000, 257, 5, 130]
+    c = _case(rows, kv, H, Hkv, hd, seed=91)
+    out, lse, err = _run(c, max_kv=claim)
+    assert err == 0
+    _check(c, out, lse)
