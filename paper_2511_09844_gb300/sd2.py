@@ -7,6 +7,7 @@ been built, importing the engine raises instead of falling back to anything else
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
 from typing import List, NamedTuple, Optional, Sequence
@@ -525,6 +526,18 @@ def _used_on(stream, *tensors):
                 t.record_stream(stream)
 
 
+@functools.lru_cache(maxsize=4096)
+def _prompt_workspace_bytes(M: int, n_seq: int, H: int, Hkv: int, hd: int, max_kv: int) -> int:
+    return load_library().sd2_attention_prompt_workspace_bytes(M, n_seq, H, Hkv, hd, max_kv)
+
+
+@functools.lru_cache(maxsize=None)
+def _word_of(index: int) -> torch.Tensor:
+    """The smallest workspace, for calls that keep no partial results in it (an error word nobody reads), so that
+    such a call need not allocate one."""
+    return torch.empty(256, dtype=torch.uint8, device=f"cuda:{index}")
+
+
 def attention_prompt(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, layer: int, cu_rows: torch.Tensor,
                      kv_len: torch.Tensor, max_kv: Optional[int] = None, return_lse: bool = False,
                      workspace: Optional[torch.Tensor] = None, err: Optional[torch.Tensor] = None, stream=None):
@@ -547,7 +560,8 @@ def attention_prompt(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, l
     out = torch.empty((M, H * hd), dtype=torch.bfloat16, device=device)
     lse = torch.empty((M, H), dtype=torch.float32, device=device) if return_lse else None
     if M:
-        ws = _workspace(workspace, lib.sd2_attention_prompt_workspace_bytes(M, n_seq, H, Hkv, hd, max_kv), device)
+        need = _prompt_workspace_bytes(M, n_seq, H, Hkv, hd, max_kv)
+        ws = _word_of(index) if workspace is None and need <= 256 else _workspace(workspace, need, device)
         _check(lib, lib.sd2_attention_prompt(q.data_ptr(), ldq, M, H, Hkv, hd, pool.data_ptr(), n_blocks, batch[0], stride,
                                              layer, batch[1], batch[2], n_seq, max_kv, out.data_ptr(),
                                              None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
