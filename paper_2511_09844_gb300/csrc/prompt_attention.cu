@@ -60,6 +60,7 @@ constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum th
 // K/V tiles from which on two slots share the work of one and join (256 sequences of 9 rows on 500 positions, 32/8 heads
 // of 64: 96 us from 4 on, 109 from 8 on; one row on 1000 positions, 32/8 heads of 128: 11.9 us from 2 on, 11.4 from 4 on)
 constexpr int kSoloTiles = 4;
+constexpr float kSumGrowth = 4096.f;       // and the sum of a tile's 128 probabilities that shows it (heads of 64)
 constexpr float kNone = -1e30f;            // the reference before a row has seen anything
 
 struct PromptArgs {
@@ -846,47 +847,78 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           unpair(add2(sum[0], sum[1]), s0, s1);
           return s0 + s1;
         };
-        // The first half is computed under the last maximum while this tile's is found; only if that has grown too
-        // much, or there is none yet, it is computed again.
         uint32_t p[2][16];
-        float part = half_exp(0, p, std::true_type());
-        const float mx = fmaxf(top[0], top[1]) * scale;
-        const bool grown = mx > m + kGrowth;
-        if (Lay::kEarly && j > j0) {         // the last P has been read (and O has its product)
-          if (!wait_warp(o_full + 8 * s, n_o++ & 1)) { ok = false; break; }
-          tc_fence_after();
-        }
-        if (__any_sync(0xffffffffu, grown)) {
+        auto put = [&](int h) {
+          st16(tp + h * 32, p[0]);
+          st16(tp + h * 32 + 16, p[1]);
+        };
+        auto hand_over = [&](int h) {        // the probabilities are there
+          st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * h);
+        };
+        auto move = [&](float mx, bool moved) {   // the reference to a row's maximum
           float f = 1.f;
-          if (grown) {
+          if (moved && mx > m) {
             f = ex2(m - mx);                 // (0 where nothing had been seen)
             m = mx;
             l *= f;
           }
           __syncwarp();
-          if (j > j0) {
+          if (j == j0) return;
 #pragma unroll 1
-            for (int c = 0; c < HD / 32; ++c) {
-              uint32_t o[32];
-              ld32(to + c * 32, o);
-              ld_wait(o);
+          for (int c = 0; c < HD / 32; ++c) {
+            uint32_t o[32];
+            ld32(to + c * 32, o);
+            ld_wait(o);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              st32(to + c * 32, o);
-            }
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            st32(to + c * 32, o);
           }
-          part = half_exp(0, p, std::false_type());
-        }
+        };
+        float part;
+        if (Lay::kEarly) {
+          // Whether a maximum has grown shows in the sum, so that it is found only then (a tenth of the instructions).
+          // P goes over in one piece: the next scores do not wait for this product.
+          bool moved = true;
+          if (j > j0) {
+            part = half_exp(0, p, std::false_type());
+            // the last P has been read (and O has its product)
+            if (!wait_warp(o_full + 8 * s, n_o++ & 1)) { ok = false; break; }
+            tc_fence_after();
+            put(0);
+            part += half_exp(1, p, std::false_type());
+            moved = part > kSumGrowth;
+          }
+          if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (h) part += half_exp(1, p, std::false_type());
-          st16(tp + h * 32, p[0]);
-          st16(tp + h * 32 + 16, p[1]);
-          if (Lay::kEarly && h == 0) continue;   // (the next scores do not wait for this product: P in one piece)
-          st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(p_full + 16 * s + (Lay::kEarly ? 0 : 8 * h));
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; i += 2)
+                top[c & 1] = fmaxf(top[c & 1], fmaxf(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])));
+            move(fmaxf(top[0], top[1]) * scale, moved);
+            part = half_exp(0, p, std::false_type());
+            put(0);
+            part += half_exp(1, p, std::false_type());
+          }
+          put(1);
+          hand_over(0);
+        } else {
+          // The first half is computed under the last reference while this tile's maximum is found; only if that has
+          // grown too much, or there is none yet, it is computed again.
+          part = half_exp(0, p, std::true_type());
+          const float mx = fmaxf(top[0], top[1]) * scale;
+          const bool moved = mx > m + kGrowth;
+          if (__any_sync(0xffffffffu, moved)) {
+            move(mx, moved);
+            part = half_exp(0, p, std::false_type());
+          }
+          put(0);
+          hand_over(0);
+          part += half_exp(1, p, std::false_type());
+          put(1);
+          hand_over(1);
         }
         l += part;
       }
