@@ -124,11 +124,12 @@ __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_desc, uint32_
       "r"(a_desc), "r"(b_desc), "r"(idesc), "r"(add), "n"(kDescHigh)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_desc, uint32_t idesc, uint32_t add) {
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_desc, uint32_t idesc, uint32_t add,
+                                       uint32_t on) {
   asm volatile(
-      "{\n .reg .pred p;\n .reg .b64 b;\n mov.b64 b, {%2, %5};\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d_tmem),
-      "r"(a_tmem), "r"(b_desc), "r"(idesc), "r"(add), "n"(kDescHigh)
+      "{\n .reg .pred p, q;\n .reg .b64 b;\n mov.b64 b, {%2, %5};\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %6, 0;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_desc), "r"(idesc), "r"(add), "n"(kDescHigh), "r"(on)
       : "memory");
 }
 
@@ -547,8 +548,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       }
     } else if (warp == 9) {
       // The products. This thread's own instructions are the limit between the waits (a turn of one slot is 1024
-      // cycles of products for hd 128, 512 for hd 64, in some 16 or 12 instructions of 10 to 40 cycles), so whole
-      // tiles of both slots run in a loop without a condition; what is left of a piece goes tile by tile.
+      // cycles of products for hd 128, 512 for hd 64, in some 16 or 12 instructions of 10 to 40 cycles): no condition
+      // between the products of one operation, and one loop for all tiles of a piece (code apart for its end would
+      // be fetched anew each time).
       if (elect_one()) {
         auto wait = [&](uint32_t bar, uint32_t parity) { return wait_spin(bar, parity, abort_flag, a.err); };
         constexpr uint32_t kSlot16 = Lay::kSlotBytes >> 4, kHalf16 = Lay::kHalf >> 4, kPage16 = Lay::kPageBytes >> 4;
@@ -568,151 +570,105 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
             mma_ss(tmem + s * kTile, a_desc + off, b_desc + off, idesc_s, kk > 0);
           }
         };
-        auto issue_o = [&](int s, uint32_t st, int part, uint32_t add) {
+        auto issue_o = [&](int s, uint32_t st, int part, uint32_t add, uint32_t on) {
           const uint32_t p = tmem + Lay::kP + s * Lay::kPStride, b_desc = v_desc + st * kSlot16;
 #pragma unroll
           for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
-            mma_ts(tmem + Lay::kO + s * HD, p + kk * 8, b_desc + kk * kPage16, idesc_o, kk > 0 ? 1u : add);
+            mma_ts(tmem + Lay::kO + s * HD, p + kk * 8, b_desc + kk * kPage16, idesc_o, kk > 0 ? 1u : add, on);
         };
         while (ok && next_work(w, wait)) {
           done_reading();
           if (w.jb >= w.je) continue;
           const int step = 1 + w.solo;
           const int last[2] = {last_tile(w, 0), last_tile(w, 1)};
-          auto active = [&](int s, int j) { return j < last[s] && (!w.solo || ((j - w.jb) & 1) == s); };
-          auto scores = [&](int s, uint32_t st) {              // S_s = Q_s K^T (columns of no page: anything, masked)
+          uint32_t st = 0;
+          auto take = [&]() {                                  // the next tile of the ring
+            st = stage(u);
+            ok = ok && full(u);
+            ++u;
+            tc_fence_after();
+          };
+          auto scores = [&](int s) {                           // S_s = Q_s K^T (columns of no page: anything, masked)
             if (Lay::kEarly) {                                 // the softmax has taken the last scores
-              if (!wait(s_free + 8 * s, (n_sc[s] & 1) ^ 1)) { ok = false; return; }
+              ok = ok && wait(s_free + 8 * s, (n_sc[s] & 1) ^ 1);
               tc_fence_after();
             }
+            if (!ok) return;
             ++n_sc[s];
             issue_s(s, q_desc + (w.solo ? 0 : s * kSlot16), st);
             mma_commit(s_full + 8 * s);
           };
-          auto values = [&](int s, int j, uint32_t st) {       // O_s += P_s V_j
+          auto values = [&](int s, int j) {                    // O_s += P_s V_j
             const uint32_t add = j >= w.jb + step ? 1u : 0u;
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {             // (the second half where the slot sees any of it)
-              if (ok && (!Lay::kEarly || part == 0)) ok = wait(p_full + 16 * s + 8 * part, n_p[s] & 1);
-              if (!ok) continue;
+            const bool more = (s ? w.end[1] : w.end[0]) - j * kTile > kTile / 2;   // the slot sees some of the second half
+            ok = ok && wait(p_full + 16 * s, n_p[s] & 1);
+            tc_fence_after();
+            if (Lay::kEarly) {
+              if (!ok) return;
+              issue_o(s, st, 0, add, 1);
+              if (more) issue_o(s, st, 1, 1, 1);
+            } else {                                           // the second half of P as it comes, without a branch
+              issue_o(s, st, 0, add, ok);
+              ok = ok && wait(p_full + 16 * s + 8, n_p[s] & 1);
               tc_fence_after();
-              if (part == 0 || (s ? w.end[1] : w.end[0]) - j * kTile > kTile / 2) issue_o(s, st, part, add);
+              issue_o(s, st, 1, 1, more && ok);
             }
             ++n_p[s];
             // O has tile j (where the next scores follow P in its columns, their barrier says so too)
-            if (ok && (Lay::kEarly || j + step >= last[s])) mma_commit(o_full + 8 * s);
+            if (Lay::kEarly || j + step >= last[s]) mma_commit(o_full + 8 * s);
           };
           if (!(ok = wait(q_full, n_q & 1))) break;
           ++n_q;
           const int head = min(step, w.je - w.jb);             // K tiles before the first V tile
-          for (int i = 0; i < head && ok; ++i, ++u) {
-            if (!(ok = full(u))) break;
-            tc_fence_after();
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-              if (ok && active(s, w.jb + i)) scores(s, stage(u));
-            mma_commit(empty0 + 8 * stage(u));
+          for (int i = 0; i < head && ok; ++i) {
+            take();
+            if ((!w.solo || i == 0) && w.jb + i < last[0]) scores(0);
+            if ((!w.solo || i == 1) && w.jb + i < last[1]) scores(1);
+            mma_commit(empty0 + 8 * st);
           }
-          if (ok && w.jb + head == w.je) mma_commit(q_empty);  // every product that reads Q has been issued
-          // tiles j whose successor is whole for both slots
-          const int whole = w.solo ? 0 : min(w.je - 1, min(w.end[0], w.end[1]) / kTile - 1);
+          if (w.jb + head == w.je) mma_commit(q_empty);        // every product that reads Q has been issued
+          bool turn[2] = {true, !w.solo};                      // the slots that tile j is for
           for (int j = w.jb; j < w.je && ok; ++j) {
-            if (j > w.jb && j < whole) {
-              uint32_t p0 = n_p[0] & 1, p1 = n_p[1] & 1, c0 = n_sc[0] & 1, c1 = n_sc[1] & 1;
-              const int n = whole - j;
-              int i = 0;
-              for (; i < n; ++i, u += 2) {
-                const uint32_t st0 = stage(u), st1 = stage(u + 1);
-                if (Lay::kEarly) {
-                  if (!full(u) || !wait(s_free, c0 ^ 1)) break;
-                  tc_fence_after();
-                  issue_s(0, q_desc, st0);
-                  mma_commit(s_full);
-                  if (!wait(s_free + 8, c1 ^ 1)) break;
-                  tc_fence_after();
-                  issue_s(1, q_desc + kSlot16, st0);
-                  mma_commit(s_full + 8);
-                  mma_commit(empty0 + 8 * st0);
-                  if (!full(u + 1)) break;
-                  if (!wait(p_full, p0)) break;
-                  tc_fence_after();
-                  issue_o(0, st1, 0, 1);
-                  issue_o(0, st1, 1, 1);
-                  mma_commit(o_full);
-                  if (!wait(p_full + 16, p1)) break;
-                  tc_fence_after();
-                  issue_o(1, st1, 0, 1);
-                  issue_o(1, st1, 1, 1);
-                  mma_commit(o_full + 8);
-                  mma_commit(empty0 + 8 * st1);
-                } else {
-                  if (!full(u) || !wait(p_full, p0)) break;
-                  tc_fence_after();
-                  issue_o(0, st0, 0, 1);
-                  if (!wait(p_full + 8, p0)) break;
-                  tc_fence_after();
-                  issue_o(0, st0, 1, 1);
-                  if (!full(u + 1)) break;
-                  tc_fence_after();
-                  issue_s(0, q_desc, st1);
-                  mma_commit(s_full);
-                  if (!wait(p_full + 16, p1)) break;
-                  tc_fence_after();
-                  issue_o(1, st0, 0, 1);
-                  if (!wait(p_full + 24, p1)) break;
-                  tc_fence_after();
-                  issue_o(1, st0, 1, 1);
-                  mma_commit(empty0 + 8 * st0);
-                  issue_s(1, q_desc + kSlot16, st1);
-                  mma_commit(s_full + 8);
-                  mma_commit(empty0 + 8 * st1);
-                }
-                p0 ^= 1; p1 ^= 1; c0 ^= 1; c1 ^= 1;
-              }
-              if (i < n) { ok = false; break; }
-#pragma unroll
-              for (int s = 0; s < 2; ++s) { n_p[s] += n; n_sc[s] += n; }
-              if (whole == w.je - 1) mma_commit(q_empty);
-              j = whole - 1;
-              continue;
-            }
             const bool k_next = j + step < w.je;
-            uint32_t k_st = 0, v_st = 0;
-            auto take = [&](uint32_t& x) {                     // the next tile of the ring
-              x = stage(u);
-              if (!full(u)) { ok = false; return; }
-              ++u;
-              tc_fence_after();
-            };
+            const bool do0 = turn[0] && j < last[0], do1 = turn[1] && j < last[1];
+            const bool next0 = turn[0] && j + step < last[0], next1 = turn[1] && j + step < last[1];
             if (Lay::kEarly) {
               if (k_next) {
-                take(k_st);
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-                  if (ok && active(s, j) && j + step < last[s]) scores(s, k_st);
-                if (ok) mma_commit(empty0 + 8 * k_st);
+                take();
+                if (next0) scores(0);
+                if (next1) scores(1);
+                mma_commit(empty0 + 8 * st);
               }
-              if (ok) take(v_st);
-#pragma unroll
-              for (int s = 0; s < 2; ++s)
-                if (ok && active(s, j)) values(s, j, v_st);
-              if (ok) mma_commit(empty0 + 8 * v_st);
+              take();
+              if (do0) values(0, j);
+              if (do1) values(1, j);
+              mma_commit(empty0 + 8 * st);
             } else {
-              bool have_k = false;
-              take(v_st);
-#pragma unroll
-              for (int s = 0; s < 2; ++s) {
-                if (!ok || !active(s, j)) continue;
-                values(s, j, v_st);
-                if (!ok || j + step >= last[s]) continue;
-                if (!have_k) take(k_st);
-                have_k = true;
-                if (ok) scores(s, k_st);
+              take();
+              const uint32_t v_st = st;
+              uint32_t k_st = v_st;
+              if (do0) values(0, j);
+              if (k_next) {
+                take();
+                k_st = st;
+                if (next0) scores(0);
               }
-              if (ok) mma_commit(empty0 + 8 * v_st);
-              if (ok && have_k) mma_commit(empty0 + 8 * k_st);
+              if (do1) {
+                st = v_st;
+                values(1, j);
+              }
+              mma_commit(empty0 + 8 * v_st);
+              if (k_next) {
+                st = k_st;
+                if (next1) scores(1);
+                mma_commit(empty0 + 8 * k_st);
+              }
             }
-            if (ok && j + step == w.je - 1) mma_commit(q_empty);
+            if (j + step == w.je - 1) mma_commit(q_empty);
+            if (w.solo) {
+              turn[0] = !turn[0];
+              turn[1] = !turn[1];
+            }
           }
         }
         mma_commit(drain);                   // all products issued by this thread have completed
