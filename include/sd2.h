@@ -388,9 +388,10 @@ sd2_status sd2_accept_logits_noalloc_check(void* stream);
  *   d_q bf16, row m's H heads of hd at d_q + m * ldq (ldq >= H * hd, a multiple of 8); d_out bf16
  *   [M, H * hd]; d_lse f32 [M, H] or null. hd 64 or 128; H a multiple of Hkv, H / Hkv <= 128.
  * A row with p < 0 sees nothing: out 0, lse -inf. Rows at or beyond d_cu_rows[n_seq] are not written.
- * Positions at or beyond min(d_kv_len[s], 16 * bt_stride) are not read, whatever their page holds;
- * those below it must hold finite values. max_kv >= every d_kv_len[s] lets the call cut long caches
- * into splits where there are few rows (it sizes the split only: a larger length is still right).
+ * Positions at or beyond min(d_kv_len[s], 16 * bt_stride) are not read, whatever their page holds; an
+ * infinity or NaN below it reaches the rows that see its position (in V: its column of them), no others.
+ * max_kv >= every d_kv_len[s] lets the call cut long caches into splits where there are few rows (it
+ * sizes the split only: a larger length is still right).
  * d_workspace: sd2_attention_prompt_workspace_bytes(M, n_seq, H, Hkv, hd, max_kv) bytes, 256-byte
  * aligned; contents need not be initialised; calls whose GPU work overlaps must not share it.
  * Errors: SD2_EINVAL (null, shape, alignment, workspace too small), SD2_ECUDA. */

@@ -70,6 +70,8 @@ struct PromptArgs {
   int kv_rows;                             // rows of map_k and map_v
   const int *table, *cu, *kv_len;
   const bf16* pool;                        // the layer's pages
+  const bf16* q;
+  long long ldq;
   bf16* out;
   float* lse;
   float *part_o, *part_lse;                // [n_splits][M * H][hd] and [n_splits][M * H] (log2)
@@ -367,6 +369,92 @@ __device__ __forceinline__ bool read_block(uint32_t answer, int& x, int& y, int&
   return ok != 0;
 }
 
+// K/V tiles slot s takes: from jb (+ 1 for slot 1 of solo work) in steps of 1 (2) below
+__device__ __forceinline__ int last_tile(const Work& w, int s) { return min(w.je, (w.end[s] + kTile - 1) / kTile); }
+
+// A masked probability is 0, and 0 times an infinity or NaN in V is NaN: in a tile that some rows of a slot see further
+// than others, such a value reaches columns of rows that do not see it. One warp computes these columns again, without
+// the tensor cores, for rows `need` of its 32 (r: this lane's query vector, m and l its reference and sum). A column
+// that the row's own positions make NaN ends early. (Inlined and fed from kept[]: looking for such columns and having
+// this at hand costs 0 to 2% of a call's time, as a function called from here 3 to 6%.)
+template <int HD>
+__device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, int s, int r, unsigned need, float m, float l) {
+  constexpr int kPer = HD / 32;
+  const int lane = threadIdx.x & 31;
+  const int* row = a.table + static_cast<size_t>(w.seq) * a.bt_stride;
+  const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD));
+  const int begin = w.jb * kTile, end = min(last_tile(w, s) * kTile, w.kv);
+  // K of a position (V: a.Hkv pages on), null where its page does not exist
+  auto keys = [&](int j) -> const bf16* {
+    const int id = row[j / kPage];
+    return id < 0 || id >= a.n_blocks ? nullptr : a.pool + ((static_cast<size_t>(id) * 2 * a.Hkv + w.hk) * kPage + j % kPage) * HD;
+  };
+  const size_t to_v = static_cast<size_t>(a.Hkv) * kPage * HD;
+  struct alignas(2 * kPer) Cols { bf16 v[kPer]; };
+  const int first = w.solo ? 0 : s * a.T, r0 = r - lane;
+#pragma unroll 1
+  for (; need; need &= need - 1) {
+    const int src = __ffs(need) - 1;
+    const float m_r = __shfl_sync(0xffffffffu, m, src), inv_r = 1.f / __shfl_sync(0xffffffffu, l, src);
+    const int t = first + (r0 + src) / a.G, see_r = min(w.pos0 + t + 1, w.kv);
+    const int token = w.row0 + t, head = w.hk * a.G + (r0 + src) % a.G;
+    const size_t item = static_cast<size_t>(token) * a.H + head;
+    float* part = a.part_o + (static_cast<size_t>(w.split) * a.M * a.H + item) * HD + lane * kPer;
+    bf16* out = a.out + item * HD + lane * kPer;
+    unsigned hidden = 0;                     // this lane's columns with such a value at a position the row does not see
+#pragma unroll 1
+    for (int j = max(see_r, begin); j < end; ++j) {
+      const bf16* k = keys(j);
+      if (!k) continue;
+      const Cols v = *reinterpret_cast<const Cols*>(k + to_v + lane * kPer);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) hidden |= (__bfloat162float(v.v[e]) * 0.f == 0.f ? 0u : 1u) << e;
+    }
+    unsigned open = 0;                       // of them, those that are NaN
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const float x = a.n_splits > 1 ? part[e] : __bfloat162float(out[e]);
+      if (hidden >> e & 1 && x != x) open |= 1u << e;
+    }
+    const unsigned mine = open;
+    const bf16* q = a.q + token * a.ldq + head * HD;
+    float acc[kPer] = {};
+#pragma unroll 1
+    for (int j0 = begin; j0 < min(end, see_r) && __any_sync(0xffffffffu, open); j0 += 32) {
+      const int n = min(32, min(end, see_r) - j0);
+      const bf16* k = lane < n ? keys(j0 + lane) : nullptr;
+      float p = 0.f;
+      if (k) {
+#pragma unroll 1
+        for (int c = 0; c < HD; c += 2) {
+          const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(q + c));
+          const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(k + c));
+          p = fmaf(x.x, y.x, fmaf(x.y, y.y, p));
+        }
+        p = ex2(p * scale - m_r);
+      }
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {
+        const float p_i = __shfl_sync(0xffffffffu, p, i);
+        const bf16* k_i = reinterpret_cast<const bf16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k), i));
+        if (!k_i) continue;
+        const Cols v = *reinterpret_cast<const Cols*>(k_i + to_v + lane * kPer);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] = fmaf(p_i, __bfloat162float(v.v[e]), acc[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < kPer; ++e)
+        if (acc[e] != acc[e]) open &= ~(1u << e);
+    }
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+      if (mine >> e & 1) {
+        if (a.n_splits > 1) part[e] = acc[e] * inv_r; else out[e] = __float2bfloat16(acc[e] * inv_r);
+      }
+  }
+  __syncwarp();
+}
+
 constexpr int kConsumers = 11;             // of a piece of work: two loaders, the MMA thread, 8 softmax warps
 
 template <int HD>
@@ -375,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
   constexpr int S = Lay::kStages, kHalves = HD / 64;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  __shared__ Work works[2];
+  __shared__ Work works[2], kept[8];       // kept: each softmax warp's, until its results are out
   __shared__ __align__(16) uint4 answer;
   __shared__ float twin[2][kTile];         // slot 1's references and sums, for slot 0 (solo work)
   __shared__ int flags[3];                 // [0] abort, [1] TMEM base, [2] the block has work of its own
@@ -445,8 +533,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
     return w.seq >= 0;
   };
   auto done_reading = [&]() { mbar_arrive(w_empty + 8 * ((n_work - 1) & 1)); };
-  // K/V tiles slot s takes: from jb (+ 1 for slot 1 of solo work) in steps of 1 (2) below
-  auto last_tile = [](const Work& w, int s) { return min(w.je, (w.end[s] + kTile - 1) / kTile); };
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
@@ -746,6 +832,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
                                                                          // does not exist need not be masked
         item = (static_cast<size_t>(w.row0) + from + t) * a.H + w.hk * a.G + g;
         split = w.split;
+        if (lane < static_cast<int>(sizeof(Work) / 4))
+          reinterpret_cast<int*>(&kept[warp])[lane] = reinterpret_cast<const int*>(&works[(n_work - 1) & 1])[lane];
         __syncwarp();
         if (lane == 0) done_reading();
       }
@@ -933,6 +1021,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       }
       const uint32_t put = panel + lane * 128, put_x = (lane & 7) * 16;
       const uint32_t get = panel + lane / 8 * 128 + ((lane % 8) ^ (lane / 8)) * 16;   // (row + 4 flips chunk bit 2)
+      uint64_t odd = 0ull;                   // 0 times every result: NaN if one is not finite
 #pragma unroll 1
       for (int c = 0; c < HD / 32; ++c) {    // (not unrolled: the code of a rare path is fetched each time)
         uint32_t o[32];
@@ -940,6 +1029,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         ld_wait(o);
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = none ? 0u : __float_as_uint(__uint_as_float(o[i]) * inv);
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) odd = fma2(pair(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), 0ull, odd);
         if (to_parts) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) st_shared(put + ((k * 16) ^ put_x), o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
@@ -971,6 +1062,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         if (to_parts) a.part_lse[part] = l2;
         else if (a.lse) a.lse[item] = l2 * 0.6931471805599453f;
       }
+      float odd0, odd1;
+      unpair(odd, odd0, odd1);
+      if (const unsigned need = __ballot_sync(0xffffffffu, valid && !(odd0 + odd1 == 0.f) && l - l == 0.f))
+        mend_rows<HD>(a, kept[warp], s, r, need, m, l);
     }
   }
   tc_fence_before();
@@ -1092,6 +1187,7 @@ cudaError_t prompt_attention(const PromptAttnArgs& p, cudaStream_t st) {
   a.M = p.M; a.H = p.H; a.Hkv = Hkv; a.G = s.G; a.T = s.T; a.n_blocks = p.kv.n_blocks; a.bt_stride = p.kv.bt_stride;
   a.n_seq = p.n_seq; a.n_splits = p.work ? s.splits : 1; a.kv_rows = p.kv.n_blocks * 2 * Hkv * kPage;
   a.table = p.kv.table; a.cu = p.cu; a.kv_len = p.kv_len; a.out = static_cast<bf16*>(p.out); a.lse = p.lse; a.err = p.err;
+  a.q = static_cast<const bf16*>(p.q); a.ldq = p.ldq;
   a.part_o = static_cast<float*>(p.work);
   a.part_lse = a.part_o + static_cast<size_t>(a.n_splits) * p.M * p.H * hd;
   a.pool = static_cast<const bf16*>(p.kv.pool) + static_cast<size_t>(p.layer) * p.kv.n_blocks * 2 * Hkv * kPage * hd;

@@ -426,3 +426,44 @@ def test_pieces_for_one_query_tile(H, Hkv, hd, claim):
     out, lse, err = _run(c, max_kv=claim)
     assert err == 0
     _check(c, out, lse)
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(8, 2, 128), (14, 2, 64), (3, 1, 128), (4, 4, 64)])
+@pytest.mark.parametrize("rows,prefix", [([300, 70], [0, 0]), ([150, 40], [333, 1000]), ([9, 12], [600, 0]),
+                                         ([33], [3333]), ([129], [127])])
+def test_values_that_only_later_rows_see(rows, prefix, H, Hkv, hd):
+    """An infinity or NaN in V reaches its own column of the rows that see its position, and nothing else, although
+    earlier rows share tiles with it."""
+    kv = [a + b for a, b in zip(rows, prefix)]
+    c = _case(rows, kv, H, Hkv, hd, seed=len(rows) + hd)
+    want = _definition(c)                             # of the finite values
+    put = []                                          # sequence, position, KV head, column, value
+    for s, (n, p) in enumerate(zip(rows, prefix)):
+        put += [(s, p + n // 2, 0, 5, float("nan")), (s, p + n - 1, Hkv - 1, hd - 1, float("inf")),
+                (s, p + 2, Hkv - 1, hd // 2, float("-inf")), (s, p + n // 3, 0, 6, float("nan"))]
+    mask = torch.zeros(sum(rows), H, hd, dtype=torch.bool)
+    spoilt = {}
+    for s, j, h, d, x in put:
+        c["pool"][c["layer"], int(c["table"][s, j // 16]), 1, h, j % 16, d] = x
+        r0, r1 = int(c["cu"][s]) + j - prefix[s], int(c["cu"][s + 1])
+        heads = slice(h * (H // Hkv), (h + 1) * (H // Hkv))
+        mask[r0:r1, heads, d] = True
+        spoilt[(s, h, d)] = (slice(r0, r1), heads, d, x)
+    out, lse, err = _run(c)
+    assert err == 0
+    assert (lse.double() - want[1]).abs().max().item() <= LSE_TOL
+    got, o, mag = (t.view(sum(rows), H, hd) for t in (out.double(), want[0], want[2]))
+    assert torch.isfinite(got[~mask]).all()
+    assert ((got - o).abs() - _bound(o, mag))[~mask].max().item() <= 1e-6
+    for a, b, d, x in spoilt.values():
+        assert torch.isnan(got[a, b, d]).all() if x != x else not torch.isfinite(got[a, b, d]).any()
+
+
+def test_values_of_no_number_everywhere():
+    """All of V NaN: every row is, and the log-sum-exps are what they were."""
+    c = _case([700, 30], [700, 90], 8, 2, 128, seed=4)
+    want = _definition(c)
+    c["pool"][c["layer"], :, 1] = float("nan")
+    out, lse, err = _run(c)
+    assert err == 0 and torch.isnan(out.float()).all()
+    assert (lse.double() - want[1]).abs().max().item() <= LSE_TOL
