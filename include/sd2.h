@@ -425,7 +425,8 @@ sd2_status sd2_pages_append(const void* d_k, int64_t ldk, const void* d_v, int64
  * New pages are the lowest free ids, granted in the order of b. When they run out (d_err bit 8) a
  * sequence without a page for its tail is cut to its whole pages, and the room ends with d_pages_out.
  * d_workspace: sd2_pages_fork_workspace_bytes(n_out, n_blocks) bytes, 256-byte aligned, contents need
- * not be initialised. Work that still reads the freed pages must come before this call on its stream. */
+ * not be initialised. n_out * bt_stride below 2^31, bt_stride at most 2^26. Work that still reads the
+ * freed pages must come before this call on its stream. */
 size_t sd2_pages_fork_workspace_bytes(int32_t n_out, int32_t n_blocks);
 sd2_status sd2_pages_fork(void* d_pool, int32_t L, int32_t n_blocks, int32_t Hkv, int32_t hd, const int32_t* d_table,
                           int32_t bt_stride, const int32_t* d_len, int32_t n_seq, const int32_t* d_parent,

@@ -150,11 +150,12 @@ __device__ __forceinline__ ForkSeq fork_seq(const ForkArgs& a, int b) {
   ForkSeq s;
   s.parent = a.parent[b];
   const int room = a.stride * kPage;
-  const int keep = a.keep ? a.keep[b] : room, grow = a.grow ? min(max(a.grow[b], 0), room) : 0;
+  const int keep = a.keep ? a.keep[b] : room;
   int len = 0;
   if (s.parent >= 0 && s.parent < a.n_seq) len = min(max(a.len[s.parent], 0), room);
   s.keep = min(max(keep, 0), len);
-  s.held = min((s.keep + grow + kPage - 1) / kPage, a.stride);
+  const int grow = a.grow ? min(max(a.grow[b], 0), room - s.keep) : 0;
+  s.held = (s.keep + grow + kPage - 1) / kPage;
   s.last = -1;
   if (s.tail()) {
     const int p = a.table[static_cast<size_t>(s.parent) * a.stride + s.full()];
@@ -649,6 +650,7 @@ sd2_status sd2_pages_fork(void* d_pool, int32_t L, int32_t n_blocks, int32_t Hkv
   if (const char* why = bad_pool(d_pool, L, n_blocks, Hkv, hd)) return fail(SD2_EINVAL, why);
   if (n_seq < 1 || n_out < 1 || bt_stride < 1 || bt_stride > (1 << 26))
     return fail(SD2_EINVAL, "need n_seq, n_out >= 1 and 1 <= bt_stride <= 2^26");
+  if (static_cast<int64_t>(n_out) * bt_stride > INT32_MAX) return fail(SD2_EINVAL, "n_out * bt_stride must be countable in 31 bits");
   if (d_table_out == d_table || d_len_out == d_len || d_ref_out == d_pinned)
     return fail(SD2_EINVAL, "outputs must not be the inputs");
   if (workspace_bytes < sd2_pages_fork_workspace_bytes(n_out, n_blocks)) return fail(SD2_EINVAL, "workspace too small");

@@ -361,3 +361,10 @@ def test_page_operators_in_a_captured_graph():
             for j in range(want[1][s]):
                 got = pool[0, c.table[s, j // 16], :, :, j % 16]
                 assert torch.equal(_bits(got), _bits(want[4][0, want[0][s][j // 16], :, :, j % 16]))
+
+
+def test_fork_with_more_room_asked_than_a_table_has():
+    top = 2 ** 31 - 1
+    f = _fork_check(_pool(2, 60, 2, 64, 9), _fresh([37, 96, 5], 6, 60, 9), [37, 96, 5], [0, 1, 2, -1, 0], keep=[top, 90, 0, 9, 20],
+                    grow=[top, top, top, 1 << 30, -top])
+    assert f.pages.tolist() == [6, 6, 6, 6, 2]

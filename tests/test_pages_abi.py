@@ -117,3 +117,13 @@ def test_binding_refuses_other_tensors(L):
                  lambda: sd2.pages_compact(pool, table, i(1), i(1, 0, 0, 0))):
         with pytest.raises(sd2.SD2Error, match="EINVAL.*pool must be"):
             call()
+
+
+def test_fork_refuses_tables_beyond_31_bits(L):
+    need = L.sd2_pages_fork_workspace_bytes(1 << 16, 64)
+
+    def call(n_out, stride):
+        return L.sd2_pages_fork(P, 2, 64, 8, 128, P, stride, P, 2, P, None, None, None, n_out, Q, Q, Q, Q, U, need, None, None)
+    assert refused(L, call(1 << 16, 1 << 15), b"n_out * bt_stride")
+    assert refused(L, call(1 << 16, (1 << 15) - 1), b"256-byte")
+    assert refused(L, call(1, (1 << 26) + 1), b"bt_stride <= 2^26")
