@@ -19,21 +19,25 @@
 //   warp 10         the work: pieces (two query tiles x their K/V tiles) are the blocks of a grid, and a
 //                   block that runs takes further ones by cluster launch control
 // TMEM: S0, S1, O0, O1 and P (over S for hd 128, where TMEM is full). Probabilities are taken relative to a
-// reference: a row's maximum over its first tile, then moved only when the maximum has grown by more than 2^8 (O is
-// then rescaled in TMEM by the softmax threads). A reference that near gives the same relative rounding (bf16 and
+// reference: a row's maximum over its first tile, then moved only when the maximum has grown by more than 2^8 (heads of
+// 128), or when a tile's probabilities add up to more than 2^12 (heads of 64: the sum is there anyway, so that the
+// maximum of a later tile is found only then: 16384 tokens 992 -> 945 us). O is then
+// rescaled in TMEM by the softmax threads. A reference that near gives the same relative rounding (bf16 and
 // fp32 are relative) and cannot overflow; from the row's own maximum, the largest probability is exactly 1, so that
 // a row that sees one position gives its value unrounded.
 //
-// Bound: the tensor cores for long prompts with heads of 128 (4 hd flops per visible pair and head), the
-// softmax's instructions with heads of 64 (about 550 per warp and 32 x 128 scores, issued every second cycle),
-// HBM for few rows on a long cache, latency for short prompts. Few rows leave SMs idle, so the positions are
-// then cut over gridDim.z splits that a second kernel joins. A piece with queries for one slot only puts both
-// slots on them, with alternate K/V tiles, and joins the two at its end (slot 0's threads read slot 1's columns).
+// Bound: the tensor cores for long prompts with heads of 128 (4 hd flops per visible pair and head), the softmax with
+// heads of 64 (a tile of both slots takes 2090 cycles, 1024 of them products: the exponential unit needs 1024, with
+// the scaling, sums and rounding 1250, the rest are barriers and the scores' and probabilities' ways through TMEM,
+// which the two warps of a scheduler come to at the same time), HBM for few rows on a long cache, latency for short
+// prompts. Few rows leave SMs idle, so the positions are then cut over gridDim.z splits that a second kernel joins. A
+// piece with queries for one slot only puts both slots on them, with alternate K/V tiles, and joins the two at its end
+// (slot 0's threads read slot 1's columns).
 //
-// Measured (GB300, 1913 TFLOP/s bf16 and 6.77 TB/s copy): one prompt of 16384, 32/8 heads of 128, 1.15-1.25 ms,
-// 1.76-1.9 PFLOP/s; four chunks of 411-777 rows on 3K-16K positions, 40/8 heads of 128, 457 us, 1.73 PFLOP/s; one
-// prompt of 16384, 32/8 heads of 64, 0.98 ms, 1.12 PFLOP/s; 6 and 17 rows on 60K and 65K positions, 95 us,
-// 5.6 TB/s; 512 rows, 32/8 heads of 128, 13 us; 37 rows 6.3 us.
+// Measured (GB300, 1913 TFLOP/s bf16 and 6.77 TB/s copy): one prompt of 16384, 32/8 heads of 128, 1.19-1.26 ms,
+// 1.75-1.85 PFLOP/s; four chunks of 411-777 rows on 3K-16K positions, 40/8 heads of 128, 461-471 us, 1.70 PFLOP/s; one
+// prompt of 16384, 32/8 heads of 64, 0.955 ms, 1.15 PFLOP/s; 6 and 17 rows on 60K and 65K positions, 95-97 us,
+// 5.5 TB/s; 512 rows, 32/8 heads of 128, 13 us; 37 rows 6.3 us.
 #include "sd2.h"
 #include "kernels.h"
 #include "tc.cuh"
@@ -58,7 +62,7 @@ constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;    // 2 x 128 x 216 + 128 x 7
 constexpr int kMaxStages = 8;
 constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum that makes O be rescaled
 // K/V tiles from which on two slots share the work of one and join (256 sequences of 9 rows on 500 positions, 32/8 heads
-// of 64: 96 us from 4 on, 109 from 8 on; one row on 1000 positions, 32/8 heads of 128: 11.9 us from 2 on, 11.4 from 4 on)
+// of 64: 94 us from 4 on, 108 from 8 on; one row on 1000 positions, 32/8 heads of 128: 11.4 us from 2 on, 11.0 from 4 on)
 constexpr int kSoloTiles = 4;
 constexpr float kSumGrowth = 4096.f;       // and the sum of a tile's 128 probabilities that shows it (heads of 64)
 constexpr float kNone = -1e30f;            // the reference before a row has seen anything
@@ -1132,10 +1136,10 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant_
 }
 
 // The grid: query tiles (an upper bound: the sequences' lengths are on the device), and splits of the
-// positions where tiles x KV heads leave SMs idle. A split keeps at least two K/V tiles (one row on 1000
-// positions: 12.7 us with two, 14.9 with four, 19.1 with eight), and as many that the partial results, f32,
-// written and read once more, are no more than the K/V bytes it reads (512 rows on no cache, 8B heads: 25 us in
-// two splits, 13.7 in one).
+// positions where tiles x KV heads leave SMs idle, one piece per SM (6 and 17 rows on 60K and 65K positions: 95 us;
+// with two pieces per SM 99, with four 110). A split keeps at least two K/V tiles (one row on 1000 positions: 11.0 us
+// with two, 14.0 with four, 15.3 with eight), and as many that the partial results, f32, written and read once more,
+// are no more than the K/V bytes it reads (512 rows on no cache, 32/8 heads of 128: 20.8 us in two splits, 13.4 in one).
 struct Shape {
   int G, T, tiles, splits;
 };
