@@ -378,12 +378,13 @@ __device__ __forceinline__ int last_tile(const Work& w, int s) { return min(w.je
 
 // A masked probability is 0, and 0 times an infinity or NaN in V is NaN: in a tile that some rows of a slot see further
 // than others, such a value reaches columns of rows that do not see it. One warp computes these columns again, without
-// the tensor cores, for rows `need` of its 32 (r: this lane's query vector, m and l its reference and sum). A column
-// that the row's own positions make NaN ends early. (Inlined and fed from kept[]: looking for such columns and having
-// this at hand costs 0 to 2% of a call's time, as a function called from here 3 to 6%.)
+// the tensor cores, for rows `need` of its 32, four at a time (r: this lane's query vector, m and l its reference and
+// sum). Columns that the rows' own positions make NaN end early. (Inlined and fed from kept[]: looking for such columns
+// and having this at hand costs 0 to 2% of a call's time, as a function called from here 3 to 6%. One such value in a
+// prompt of 16384, 32/8 heads of 128: 13 ms instead of 1.3; one in every 128 positions, each in another column: 140 ms.)
 template <int HD>
 __device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, int s, int r, unsigned need, float m, float l) {
-  constexpr int kPer = HD / 32;
+  constexpr int kPer = HD / 32, kRows = 4;
   const int lane = threadIdx.x & 31;
   const int* row = a.table + static_cast<size_t>(w.seq) * a.bt_stride;
   const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD));
@@ -397,64 +398,101 @@ __device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, in
   struct alignas(2 * kPer) Cols { bf16 v[kPer]; };
   const int first = w.solo ? 0 : s * a.T, r0 = r - lane;
 #pragma unroll 1
-  for (; need; need &= need - 1) {
-    const int src = __ffs(need) - 1;
-    const float m_r = __shfl_sync(0xffffffffu, m, src), inv_r = 1.f / __shfl_sync(0xffffffffu, l, src);
-    const int t = first + (r0 + src) / a.G, see_r = min(w.pos0 + t + 1, w.kv);
-    const int token = w.row0 + t, head = w.hk * a.G + (r0 + src) % a.G;
-    const size_t item = static_cast<size_t>(token) * a.H + head;
-    float* part = a.part_o + (static_cast<size_t>(w.split) * a.M * a.H + item) * HD + lane * kPer;
-    bf16* out = a.out + item * HD + lane * kPer;
-    unsigned hidden = 0;                     // this lane's columns with such a value at a position the row does not see
-#pragma unroll 1
-    for (int j = max(see_r, begin); j < end; ++j) {
-      const bf16* k = keys(j);
-      if (!k) continue;
-      const Cols v = *reinterpret_cast<const Cols*>(k + to_v + lane * kPer);
+  while (need) {
+    float m_r[kRows], inv_r[kRows], acc[kRows][kPer] = {};
+    int see_r[kRows], see_min = INT_MAX, see_max = 0;
+    const bf16* q[kRows];
+    size_t item[kRows];
+    int src = 0;
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) hidden |= (__bfloat162float(v.v[e]) * 0.f == 0.f ? 0u : 1u) << e;
+    for (int k = 0; k < kRows; ++k) {        // (the last row again where there are no four)
+      if (need) src = __ffs(need) - 1;
+      need &= need - 1;
+      m_r[k] = __shfl_sync(0xffffffffu, m, src);
+      inv_r[k] = 1.f / __shfl_sync(0xffffffffu, l, src);
+      const int t = first + (r0 + src) / a.G, head = w.hk * a.G + (r0 + src) % a.G;
+      see_r[k] = min(w.pos0 + t + 1, w.kv);
+      see_min = min(see_min, see_r[k]);
+      see_max = max(see_max, see_r[k]);
+      q[k] = a.q + (w.row0 + t) * a.ldq + head * HD;
+      item[k] = static_cast<size_t>(w.row0 + t) * a.H + head;
     }
-    unsigned open = 0;                       // of them, those that are NaN
+    auto part = [&](int k) { return a.part_o + (static_cast<size_t>(w.split) * a.M * a.H + item[k]) * HD + lane * kPer; };
+    auto out = [&](int k) { return a.out + item[k] * HD + lane * kPer; };
+    unsigned mine = 0;                       // this lane's columns with such a value at a position the row does not see
+#pragma unroll 1
+    for (int j = max(see_min, begin); j < end; ++j) {
+      const bf16* key = keys(j);
+      if (!key) continue;
+      const Cols v = *reinterpret_cast<const Cols*>(key + to_v + lane * kPer);
+      unsigned odd = 0;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      const float x = a.n_splits > 1 ? part[e] : __bfloat162float(out[e]);
-      if (hidden >> e & 1 && x != x) open |= 1u << e;
+      for (int e = 0; e < kPer; ++e) odd |= (__bfloat162float(v.v[e]) * 0.f == 0.f ? 0u : 1u) << e;
+#pragma unroll
+      for (int k = 0; k < kRows; ++k)
+        if (j >= see_r[k]) mine |= odd << (k * kPer);
     }
-    const unsigned mine = open;
-    const bf16* q = a.q + token * a.ldq + head * HD;
-    float acc[kPer] = {};
+    unsigned now = 0;                        // of them, those that are NaN
+#pragma unroll
+    for (int k = 0; k < kRows; ++k)
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const float x = a.n_splits > 1 ? part(k)[e] : __bfloat162float(out(k)[e]);
+        if (x != x) now |= 1u << (k * kPer + e);
+      }
+    mine &= now;
+    unsigned open = mine;
+    const int limit = min(end, see_max);
 #pragma unroll 1
-    for (int j0 = begin; j0 < min(end, see_r) && __any_sync(0xffffffffu, open); j0 += 32) {
-      const int n = min(32, min(end, see_r) - j0);
-      const bf16* k = lane < n ? keys(j0 + lane) : nullptr;
-      float p = 0.f;
-      if (k) {
-#pragma unroll 1
-        for (int c = 0; c < HD; c += 2) {
-          const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(q + c));
-          const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(k + c));
-          p = fmaf(x.x, y.x, fmaf(x.y, y.y, p));
+    for (int j0 = begin; j0 < limit && __any_sync(0xffffffffu, open); j0 += 32) {
+      const int n = min(32, limit - j0);
+      const bf16* key = lane < n ? keys(j0 + lane) : nullptr;
+      float p[kRows] = {};
+      if (key) {
+#pragma unroll 2
+        for (int c = 0; c < HD; c += 8) {
+          const uint4 y = *reinterpret_cast<const uint4*>(key + c);
+          const __nv_bfloat162* y2 = reinterpret_cast<const __nv_bfloat162*>(&y);
+#pragma unroll
+          for (int k = 0; k < kRows; ++k) {
+            const uint4 x = *reinterpret_cast<const uint4*>(q[k] + c);
+            const __nv_bfloat162* x2 = reinterpret_cast<const __nv_bfloat162*>(&x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 u = __bfloat1622float2(x2[e]), v = __bfloat1622float2(y2[e]);
+              p[k] = fmaf(u.x, v.x, fmaf(u.y, v.y, p[k]));
+            }
+          }
         }
-        p = ex2(p * scale - m_r);
       }
-#pragma unroll 1
-      for (int i = 0; i < n; ++i) {
-        const float p_i = __shfl_sync(0xffffffffu, p, i);
-        const bf16* k_i = reinterpret_cast<const bf16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k), i));
-        if (!k_i) continue;
-        const Cols v = *reinterpret_cast<const Cols*>(k_i + to_v + lane * kPer);
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] = fmaf(p_i, __bfloat162float(v.v[e]), acc[e]);
+      for (int k = 0; k < kRows; ++k) p[k] = ex2(p[k] * scale - m_r[k]);
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) {
+        const bf16* k_i = reinterpret_cast<const bf16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(key), i));
+        Cols v = {};
+        if (k_i) v = *reinterpret_cast<const Cols*>(k_i + to_v + lane * kPer);
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+          const float p_i = __shfl_sync(0xffffffffu, p[k], i);
+          if (j0 + i >= see_r[k]) continue;
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) acc[k][e] = fmaf(p_i, __bfloat162float(v.v[e]), acc[k][e]);
+        }
       }
+#pragma unroll
+      for (int k = 0; k < kRows; ++k)
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+          if (acc[k][e] != acc[k][e]) open &= ~(1u << (k * kPer + e));
+    }
+#pragma unroll
+    for (int k = 0; k < kRows; ++k)
 #pragma unroll
       for (int e = 0; e < kPer; ++e)
-        if (acc[e] != acc[e]) open &= ~(1u << e);
-    }
-#pragma unroll
-    for (int e = 0; e < kPer; ++e)
-      if (mine >> e & 1) {
-        if (a.n_splits > 1) part[e] = acc[e] * inv_r; else out[e] = __float2bfloat16(acc[e] * inv_r);
-      }
+        if (mine >> (k * kPer + e) & 1) {
+          if (a.n_splits > 1) part(k)[e] = acc[k][e] * inv_r[k]; else out(k)[e] = __float2bfloat16(acc[k][e] * inv_r[k]);
+        }
   }
   __syncwarp();
 }
