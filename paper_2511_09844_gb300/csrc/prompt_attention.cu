@@ -747,18 +747,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           };
           if (!(ok = wait(q_full, n_q & 1))) break;
           ++n_q;
-          const int head = min(step, w.je - w.jb);             // K tiles before the first V tile
-          for (int i = 0; i < head && ok; ++i) {
-            take();
-            if ((!w.solo || i == 0) && w.jb + i < last[0]) scores(0);
-            if ((!w.solo || i == 1) && w.jb + i < last[1]) scores(1);
-            mma_commit(empty0 + 8 * st);
-          }
-          if (w.jb + head == w.je) mma_commit(q_empty);        // every product that reads Q has been issued
           bool turn[2] = {true, !w.solo};                      // the slots that tile j is for
-          for (int j = w.jb; j < w.je && ok; ++j) {
-            const bool k_next = j + step < w.je;
-            const bool do0 = turn[0] && j < last[0], do1 = turn[1] && j < last[1];
+          for (int j = w.jb - step; j < w.je && ok; ++j) {     // (the first round or two: scores only)
+            const bool v_now = j >= w.jb, k_next = j + step < w.je;
+            const bool do0 = v_now && turn[0] && j < last[0], do1 = v_now && turn[1] && j < last[1];
             const bool next0 = turn[0] && j + step < last[0], next1 = turn[1] && j + step < last[1];
             if (Lay::kEarly) {
               if (k_next) {
@@ -767,32 +759,36 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
                 if (next1) scores(1);
                 mma_commit(empty0 + 8 * st);
               }
-              take();
-              if (do0) values(0, j);
-              if (do1) values(1, j);
-              mma_commit(empty0 + 8 * st);
+              if (v_now) {
+                take();
+                if (do0) values(0, j);
+                if (do1) values(1, j);
+                mma_commit(empty0 + 8 * st);
+              }
             } else {
-              take();
-              const uint32_t v_st = st;
-              uint32_t k_st = v_st;
-              if (do0) values(0, j);
+              uint32_t v_st = 0, k_st = 0;
+              if (v_now) {
+                take();
+                v_st = st;
+                if (do0) values(0, j);
+              }
               if (k_next) {
                 take();
                 k_st = st;
                 if (next0) scores(0);
               }
-              if (do1) {
+              if (v_now) {
                 st = v_st;
-                values(1, j);
+                if (do1) values(1, j);
+                mma_commit(empty0 + 8 * st);
               }
-              mma_commit(empty0 + 8 * v_st);
               if (k_next) {
                 st = k_st;
                 if (next1) scores(1);
-                mma_commit(empty0 + 8 * k_st);
+                mma_commit(empty0 + 8 * st);
               }
             }
-            if (j + step == w.je - 1) mma_commit(q_empty);
+            if (j + step == w.je - 1) mma_commit(q_empty);     // every product that reads Q has been issued
             if (w.solo) {
               turn[0] = !turn[0];
               turn[1] = !turn[1];
@@ -900,6 +896,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int n = vis - c * 32;
+            if (!__any_sync(0xffffffffu, n < 32)) continue;
             const uint32_t seen = n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
 #pragma unroll
             for (int i = 0; i < 32; ++i)
