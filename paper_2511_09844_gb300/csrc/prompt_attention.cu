@@ -98,7 +98,7 @@ struct Layout {
 };
 
 // One piece of work: two query tiles (slots) of a sequence and KV head against some of its K/V tiles.
-struct Work {
+struct alignas(16) Work {
   int seq, hk, split;                      // seq < 0: no more work
   int row0, pos0, kv;                      // first packed row and its position, positions that exist
   int solo;                                // both slots hold the same tokens, take K/V tiles in turn and are joined
@@ -855,7 +855,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
     bool ok = true;
     while (ok) {
       int j0, je_s, step, see_r, split, solo;
-      size_t item;
+      int item;                              // (row, head), -1 where the row does not exist
       bool valid;
       {
         Work w;
@@ -868,7 +868,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
         valid = t < (s ? w.tokens[1] : w.tokens[0]);
         see_r = valid ? min(w.pos0 + from + t + 1, w.kv) : INT_MAX;   // this row sees positions [0, see_r); one that
                                                                          // does not exist need not be masked
-        item = (static_cast<size_t>(w.row0) + from + t) * a.H + w.hk * a.G + g;
+        item = valid ? (w.row0 + from + t) * a.H + w.hk * a.G + g : -1;
         split = w.split;
         if (lane < static_cast<int>(sizeof(Work) / 4))
           reinterpret_cast<int*>(&kept[warp])[lane] = reinterpret_cast<const int*>(&works[(n_work - 1) & 1])[lane];
@@ -1042,21 +1042,19 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       }
       const bool none = l == 0.f;            // nothing seen (a NaN is passed on)
       const float inv = 1.f / l;
-      const size_t n_items = static_cast<size_t>(a.M) * a.H;
-      const size_t part = static_cast<size_t>(split) * n_items + item;
       // The results leave through a panel of 32 rows x 128 bytes (16-byte chunks rotated by the row), so that a store
       // covers whole rows: straight from the lanes, each with a row of its own, every 16 bytes took a pass of the
       // store path (7000 cycles a piece).
       const bool to_parts = a.n_splits > 1;
-      const unsigned rows_valid = __ballot_sync(0xffffffffu, valid);
-      const uint64_t row_ptr = to_parts ? reinterpret_cast<uint64_t>(a.part_o + part * HD)
-                                        : reinterpret_cast<uint64_t>(a.out + item * HD);
+      const size_t part0 = static_cast<size_t>(split) * a.M * a.H;
+      unsigned char* const base = (to_parts ? reinterpret_cast<unsigned char*>(a.part_o + part0 * HD)
+                                            : reinterpret_cast<unsigned char*>(a.out)) + lane % 8 * 16;
+      const unsigned row_bytes = to_parts ? HD * 4 : HD * 2;
       unsigned char* dst[8];                 // lane's 16 bytes of rows lane / 8, + 4, + 8 ..
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int row = i * 4 + lane / 8;
-        const uint64_t at = __shfl_sync(0xffffffffu, static_cast<unsigned long long>(row_ptr), row);
-        dst[i] = rows_valid >> row & 1 ? reinterpret_cast<unsigned char*>(at) + lane % 8 * 16 : nullptr;
+        const int at = __shfl_sync(0xffffffffu, item, i * 4 + lane / 8);
+        dst[i] = at < 0 ? nullptr : base + static_cast<size_t>(at) * row_bytes;
       }
       const uint32_t put = panel + lane * 128, put_x = (lane & 7) * 16;
       const uint32_t get = panel + lane / 8 * 128 + ((lane % 8) ^ (lane / 8)) * 16;   // (row + 4 flips chunk bit 2)
@@ -1098,7 +1096,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       }
       if (valid) {
         const float l2 = none ? -INFINITY : m + log2f(l);
-        if (to_parts) a.part_lse[part] = l2;
+        if (to_parts) a.part_lse[part0 + item] = l2;
         else if (a.lse) a.lse[item] = l2 * 0.6931471805599453f;
       }
       float odd0, odd1;
