@@ -27,7 +27,7 @@
 // a row that sees one position gives its value unrounded.
 //
 // Bound: the tensor cores for long prompts with heads of 128 (4 hd flops per visible pair and head), the softmax with
-// heads of 64 (a tile of both slots takes 2090 cycles, 1024 of them products: the exponential unit needs 1024, with
+// heads of 64 (a tile of both slots takes 2050 cycles, 1024 of them products: the exponential unit needs 1024, with
 // the scaling, sums and rounding 1250, the rest are barriers and the scores' and probabilities' ways through TMEM,
 // which the two warps of a scheduler come to at the same time), HBM for few rows on a long cache, latency for short
 // prompts. Few rows leave SMs idle, so the positions are then cut over gridDim.z splits that a second kernel joins. A
@@ -35,8 +35,8 @@
 // (slot 0's threads read slot 1's columns).
 //
 // Measured (GB300, 1913 TFLOP/s bf16 and 6.77 TB/s copy): one prompt of 16384, 32/8 heads of 128, 1.19-1.26 ms,
-// 1.75-1.85 PFLOP/s; four chunks of 411-777 rows on 3K-16K positions, 40/8 heads of 128, 461-471 us, 1.70 PFLOP/s; one
-// prompt of 16384, 32/8 heads of 64, 0.955 ms, 1.15 PFLOP/s; 6 and 17 rows on 60K and 65K positions, 95-97 us,
+// 1.75-1.85 PFLOP/s; four chunks of 411-777 rows on 3K-16K positions, 40/8 heads of 128, 459-465 us, 1.71 PFLOP/s; one
+// prompt of 16384, 32/8 heads of 64, 0.935 ms, 1.18 PFLOP/s; 6 and 17 rows on 60K and 65K positions, 95-97 us,
 // 5.5 TB/s; 512 rows, 32/8 heads of 128, 13 us; 37 rows 6.3 us.
 #include "sd2.h"
 #include "kernels.h"
@@ -62,7 +62,7 @@ constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;    // 2 x 128 x 216 + 128 x 7
 constexpr int kMaxStages = 8;
 constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum that makes O be rescaled
 // K/V tiles from which on two slots share the work of one and join (256 sequences of 9 rows on 500 positions, 32/8 heads
-// of 64: 94 us from 4 on, 108 from 8 on; one row on 1000 positions, 32/8 heads of 128: 11.4 us from 2 on, 11.0 from 4 on)
+// of 64: 92 us from 4 on, 106 from 8 on; one row on 1000 positions, 32/8 heads of 128: 11.4 us from 2 on, 11.0 from 4 on)
 constexpr int kSoloTiles = 4;
 constexpr float kSumGrowth = 4096.f;       // and the sum of a tile's 128 probabilities that shows it (heads of 64)
 constexpr float kNone = -1e30f;            // the reference before a row has seen anything
