@@ -61,9 +61,9 @@ constexpr int kThreads = 384;             // three warpgroups: 168 registers eac
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;    // 2 x 128 x 216 + 128 x 72 = 384 x 168
 constexpr int kMaxStages = 8;
 constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum that makes O be rescaled
-// K/V tiles from which on two slots share the work of one and join (256 sequences of 9 rows on 500 positions, 32/8 heads
-// of 64: 92 us from 4 on, 106 from 8 on; one row on 1000 positions, 32/8 heads of 128: 11.4 us from 2 on, 11.0 from 4 on)
-constexpr int kSoloTiles = 4;
+// K/V tiles from which on two slots share the work of one and join (64 sequences of 20 rows on 300 positions, 32/8 heads
+// of 128: 31.7 us from 3 on, 34.2 from 4 on; one row on 1000 positions: 11.7 us from 2 on, 11.4 from 3, 11.3 from 4)
+constexpr int kSoloTiles = 3;
 constexpr float kSumGrowth = 4096.f;       // and the sum of a tile's 128 probabilities that shows it (heads of 64)
 constexpr float kNone = -1e30f;            // the reference before a row has seen anything
 

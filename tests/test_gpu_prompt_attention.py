@@ -467,3 +467,14 @@ def test_values_of_no_number_everywhere():
     out, lse, err = _run(c)
     assert err == 0 and torch.isnan(out.float()).all()
     assert (lse.double() - want[1]).abs().max().item() <= LSE_TOL
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(8, 2, 128), (14, 2, 64), (128, 1, 64)])
+@pytest.mark.parametrize("tiles", [1, 2, 3, 4, 5])
+def test_few_rows_on_each_number_of_tiles(H, Hkv, hd, tiles):
+    """Rows for one slot: from some number of K/V tiles on two slots share them."""
+    kv = [128 * tiles - 127, 128 * tiles - 1, 128 * tiles]
+    c = _case([1, min(5, kv[1]), 1], kv, H, Hkv, hd, seed=tiles)
+    out, lse, err = _run(c, max_kv=kv[2])
+    assert err == 0
+    _check(c, out, lse)
