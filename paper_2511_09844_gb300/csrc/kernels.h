@@ -6,6 +6,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <utility>
 
 namespace sd2 {
@@ -50,6 +51,18 @@ cudaError_t launch_pdl_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, 
   cfg.attrs = attr;
   cfg.numAttrs = n;
   return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
+// Lets `kernel` be launched with up to `bytes` of dynamic shared memory; `done` (the kernel's own, static) notes the
+// devices for which that has been set. Without it 48 KB are there for static and dynamic memory together.
+template <typename... KArgs>
+cudaError_t allow_smem(void (*kernel)(KArgs...), int bytes, std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev <= 63 && done.load() >> dev & 1)) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev <= 63) done.fetch_or(1ull << dev);
+  return e;
 }
 
 // ---------------------------------------------------------------- weight-streaming GEMM

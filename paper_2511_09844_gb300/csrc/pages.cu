@@ -14,6 +14,7 @@
 #include "kernels.h"
 
 #include <algorithm>
+#include <atomic>
 #include <string>
 
 namespace sd2 {
@@ -672,13 +673,10 @@ sd2_status sd2_pages_fork(void* d_pool, int32_t L, int32_t n_blocks, int32_t Hkv
   const bool one = n_out <= kOneSeqs && n_blocks <= kOnePages && static_cast<int64_t>(n_out) * bt_stride <= kOneEntries;
   cudaError_t e;
   if (one) {
-    const size_t smem = one_block_smem(n_out, n_blocks);
-    if (smem > 48 * 1024) {
-      e = cudaFuncSetAttribute(fork_one_block_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               static_cast<int>(one_block_smem(kOneSeqs, kOnePages)));
-      if (e != cudaSuccess) return launched(e, "fork plan");
-    }
-    fork_one_block_kernel<<<1, kOneThreads, smem, st>>>(a);
+    static std::atomic<unsigned long long> set{0};
+    e = allow_smem(fork_one_block_kernel, static_cast<int>(one_block_smem(kOneSeqs, kOnePages)), set);
+    if (e != cudaSuccess) return launched(e, "fork plan");
+    fork_one_block_kernel<<<1, kOneThreads, one_block_smem(n_out, n_blocks), st>>>(a);
   } else {
     e = cudaMemsetAsync(a.count, 0, (2 * padded + 4) * sizeof(int), st);
     if (e != cudaSuccess) return launched(e, "fork workspace");

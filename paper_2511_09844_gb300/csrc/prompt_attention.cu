@@ -1192,16 +1192,9 @@ Shape shape_of(int M, int n_seq, int H, int Hkv, int hd, int max_kv) {
 template <int HD>
 cudaError_t launch(const PromptArgs& a, int tiles, cudaStream_t st) {
   constexpr int smem = Layout<HD>::kSmem;
-  // (set once for every device this process uses)
   static std::atomic<unsigned long long> set{0};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  cudaError_t e = allow_smem(prompt_attention_kernel<HD>, smem, set);
   if (e != cudaSuccess) return e;
-  if (dev > 63 || !(set.load() >> dev & 1)) {
-    e = cudaFuncSetAttribute(prompt_attention_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-    if (dev <= 63) set.fetch_or(1ull << dev);
-  }
   prompt_attention_kernel<HD><<<dim3(a.Hkv * tiles, 1, a.n_splits), kThreads, smem, st>>>(a);
   if ((e = cudaGetLastError()) != cudaSuccess || a.n_splits == 1) return e;
   const long long items = static_cast<long long>(a.M) * a.H;

@@ -1,10 +1,13 @@
 """Appending to, forking and compacting the shared paged cache against plain Python: whole numbers and
 copied rows, so everything has to be equal."""
 import random
+import subprocess
+import sys
 
 import pytest
 import torch
 
+from conftest import ROOT
 from paper_2511_09844_gb300 import sd2
 
 pytestmark = pytest.mark.gpu
@@ -368,3 +371,18 @@ def test_fork_with_more_room_asked_than_a_table_has():
     f = _fork_check(_pool(2, 60, 2, 64, 9), _fresh([37, 96, 5], 6, 60, 9), [37, 96, 5], [0, 1, 2, -1, 0], keep=[top, 90, 0, 9, 20],
                     grow=[top, top, top, 1 << 30, -top])
     assert f.pages.tolist() == [6, 6, 6, 6, 2]
+
+
+def test_fork_at_the_limit_of_default_shared_memory():
+    """Plans whose counters come to just under and just over what a block gets without asking: each the first fork of
+    its process, since a larger one raises the limit for those after it."""
+    sizes = [(4, 4079), (4, 4080), (4, 4088), (4, 4089), (30, 4032), (512, 3072)]
+    script = ("import sys; sys.path[:0] = ['tests', '.']\n"
+              "import test_gpu_pages as t\n"
+              "n, blocks = int(sys.argv[1]), int(sys.argv[2])\n"
+              "t._fork_check(t._pool(1, blocks, 1, 8), t._fresh([20], 2, blocks, 1), [20], [0] * n, grow=[3] * n)\n")
+    procs = [subprocess.Popen([sys.executable, "-c", script, str(n), str(m)], cwd=ROOT, stdout=subprocess.PIPE,
+                              stderr=subprocess.STDOUT, text=True) for n, m in sizes]
+    for size, p in zip(sizes, procs):
+        out, _ = p.communicate(timeout=300)
+        assert p.returncode == 0, (size, out)
