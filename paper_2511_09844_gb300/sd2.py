@@ -511,19 +511,24 @@ def _error_word(err: Optional[torch.Tensor], index: int):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream_handle(stream, index: int) -> int:
-    if stream is not None:
-        return stream.cuda_stream
+def _stream_handle(index: int) -> int:
     return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
 
 
-def _used_on(stream, *tensors):
-    """Tensors allocated here for work on a stream that is not the current one: their memory may be reused
-    only after that work."""
-    if stream is not None:
-        for t in tensors:
+def _within(stream, workspace: Optional[torch.Tensor], call, *args, **kw):
+    """A call on a given stream: made with that stream current, so that what it allocates is that stream's memory (a
+    block of the caller's stream may still be written by work that is pending there). The caller's workspace and
+    the outputs may be dropped at any time: they are kept until the work of the other stream is done."""
+    caller = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        out = call(*args, **kw)
+    if caller != stream:
+        for t in out if isinstance(out, tuple) else (out,):
             if t is not None:
-                t.record_stream(stream)
+                t.record_stream(caller)
+        if workspace is not None:
+            workspace.record_stream(stream)
+    return out
 
 
 @functools.lru_cache(maxsize=4096)
@@ -546,6 +551,9 @@ def attention_prompt(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, l
     cu_rows int32 [n_seq + 1]; kv_len int32 [n_seq], the cached length with the new rows; max_kv a host
     bound of it (default: the table's room). Returns bf16 [M, H * hd], with f32 [M, H] log-sum-exps if
     `return_lse`. Rows of no sequence are left unwritten."""
+    if stream is not None:
+        return _within(stream, workspace, attention_prompt, q, pool, table, layer, cu_rows, kv_len, max_kv, return_lse,
+                       workspace, err)
     lib = load_library()
     L, n_blocks, Hkv, hd, index = _pool_shape(pool)
     device = pool.device
@@ -565,8 +573,7 @@ def attention_prompt(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, l
         _check(lib, lib.sd2_attention_prompt(q.data_ptr(), ldq, M, H, Hkv, hd, pool.data_ptr(), n_blocks, batch[0], stride,
                                              layer, batch[1], batch[2], n_seq, max_kv, out.data_ptr(),
                                              None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
-                                             _error_word(err, index), _stream_handle(stream, index)))
-        _used_on(stream, out, lse, ws)
+                                             _error_word(err, index), _stream_handle(index)))
     return (out, lse) if return_lse else out
 
 
@@ -575,6 +582,8 @@ def pages_append(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor, table: to
     """Write packed K/V rows to their pages of one layer (sd2_pages_append). k, v [M, Hkv, hd], f32 or
     bf16, any row stride (views of a fused projection's output will do); the batch as in
     attention_prompt."""
+    if stream is not None:
+        return _within(stream, None, pages_append, k, v, pool, table, layer, cu_rows, kv_len, err)
     lib = load_library()
     L, n_blocks, Hkv, hd, index = _pool_shape(pool)
     n_seq, stride = _table_shape(table)
@@ -590,7 +599,7 @@ def pages_append(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor, table: to
         _check(lib, lib.sd2_pages_append(k.data_ptr(), ldk, v.data_ptr(), ldv,
                                          DTYPE_BF16 if k.dtype == torch.bfloat16 else DTYPE_F32, k.shape[0], Hkv, hd,
                                          pool.data_ptr(), n_blocks, batch[0], stride, layer, batch[1], batch[2], n_seq,
-                                         _error_word(err, index), _stream_handle(stream, index)))
+                                         _error_word(err, index), _stream_handle(index)))
 
 
 class ForkedPages(NamedTuple):
@@ -607,6 +616,8 @@ def pages_fork(pool: torch.Tensor, table: torch.Tensor, length: torch.Tensor, pa
     """A new batch out of an old one (sd2_pages_fork): sequence b continues old sequence parent[b] (-1:
     none) after its first keep[b] positions, with room for grow[b] more. Sequences that no parent entry
     names give up their pages; whole pages are shared, shared tails copied."""
+    if stream is not None:
+        return _within(stream, workspace, pages_fork, pool, table, length, parent, keep, grow, pinned, workspace, err)
     lib = load_library()
     L, n_blocks, Hkv, hd, index = _pool_shape(pool)
     device = pool.device
@@ -624,8 +635,7 @@ def pages_fork(pool: torch.Tensor, table: torch.Tensor, length: torch.Tensor, pa
     _check(lib, lib.sd2_pages_fork(pool.data_ptr(), L, n_blocks, Hkv, hd, ins[0], stride, ins[1], n_seq, ins[2], ins[3],
                                    ins[4], ins[5], n, f.table.data_ptr(), f.length.data_ptr(), f.pages.data_ptr(),
                                    f.ref.data_ptr(), ws.data_ptr(), ws.nbytes, _error_word(err, index),
-                                   _stream_handle(stream, index)))
-    _used_on(stream, *f, ws)
+                                   _stream_handle(index)))
     return f
 
 
@@ -641,6 +651,8 @@ def pages_compact(pool: torch.Tensor, table: torch.Tensor, pages: torch.Tensor, 
                   stream=None) -> CompactedPages:
     """Move the pool's live pages (ref > 0) to the lowest ids (sd2_pages_compact); `pages` [n_seq] are the
     entries in use of each table row."""
+    if stream is not None:
+        return _within(stream, workspace, pages_compact, pool, table, pages, ref, workspace, err)
     lib = load_library()
     L, n_blocks, Hkv, hd, index = _pool_shape(pool)
     device = pool.device
@@ -654,6 +666,5 @@ def pages_compact(pool: torch.Tensor, table: torch.Tensor, pages: torch.Tensor, 
     ws = _workspace(workspace, lib.sd2_pages_compact_workspace_bytes(n_blocks), device)
     _check(lib, lib.sd2_pages_compact(pool.data_ptr(), L, n_blocks, Hkv, hd, ins[0], stride, ins[1], n_seq, ins[2],
                                       c.table.data_ptr(), c.ref.data_ptr(), c.map.data_ptr(), c.n_live.data_ptr(),
-                                      ws.data_ptr(), ws.nbytes, _error_word(err, index), _stream_handle(stream, index)))
-    _used_on(stream, *c, ws)
+                                      ws.data_ptr(), ws.nbytes, _error_word(err, index), _stream_handle(index)))
     return c

@@ -478,3 +478,25 @@ def test_few_rows_on_each_number_of_tiles(H, Hkv, hd, tiles):
     out, lse, err = _run(c, max_kv=kv[2])
     assert err == 0
     _check(c, out, lse)
+
+
+def test_a_block_freed_behind_pending_work_is_not_taken_on_another_stream():
+    """Memory that the current stream still writes when a call on another stream needs as much: the call's own results
+    stay what they are."""
+    c = _case([300, 45], [300, 700], 8, 2, 128, seed=51)
+    out, lse, _ = _run(c)
+    d = {k: v.cuda() for k, v in c.items() if isinstance(v, torch.Tensor)}
+    side = torch.cuda.Stream()
+    busy = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        block, stats = torch.empty(345, 1024, dtype=torch.bfloat16, device="cuda"), torch.empty(345, 8, device="cuda")
+        for _ in range(20):
+            busy = busy @ busy                                   # some milliseconds of work before the blocks are written
+        block.fill_(7.0)
+        stats.fill_(7.0)
+        del block, stats
+        o, l = sd2.attention_prompt(d["q"], d["pool"], d["table"], c["layer"], d["cu"], d["kv_len"], max_kv=700,
+                                    return_lse=True, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(o.cpu(), out) and torch.equal(l.cpu(), lse)

@@ -127,3 +127,85 @@ def test_fork_refuses_tables_beyond_31_bits(L):
     assert refused(L, call(1 << 16, 1 << 15), b"n_out * bt_stride")
     assert refused(L, call(1 << 16, (1 << 15) - 1), b"256-byte")
     assert refused(L, call(1, (1 << 26) + 1), b"bt_stride <= 2^26")
+
+
+class _Recorded(torch.Tensor):
+    """A tensor that notes the streams it is said to be used on."""
+
+    def record_stream(self, stream):
+        self.__dict__.setdefault("streams", []).append(stream)
+
+
+def _host_calls(monkeypatch, current):
+    """The four calls of the binding on host tensors and a library that does nothing: (calls by name, the stream that was
+    current at each allocation, the handles that the library got). `current` is a one-element list, the current stream."""
+    made, handles = [], []
+
+    class Lib:
+        def __getattr__(self, name):
+            if name.endswith("workspace_bytes"):
+                return lambda *a: 4096
+            return lambda *a: handles.append(a[-1]) or 0
+
+    class Use:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.stream
+
+        def __exit__(self, *a):
+            current[0] = self.before
+
+    def empty(*a, **kw):
+        made.append(current[0])
+        return host_empty(*a, **kw).as_subclass(_Recorded)
+
+    host_empty = torch.empty
+    monkeypatch.setattr(torch, "empty", empty)
+    monkeypatch.setattr(torch.cuda, "stream", Use)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: current[0])
+    monkeypatch.setattr(sd2, "_raw_stream", None)
+    monkeypatch.setattr(sd2, "load_library", lambda: Lib())
+    monkeypatch.setattr(sd2, "_pool_shape", lambda pool: (1, 4, 2, 64, -1))
+    monkeypatch.setattr(sd2, "_prompt_workspace_bytes", lambda *a: 4096)
+    i = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    pool = torch.zeros(1, 4, 2, 2, 16, 64, dtype=torch.bfloat16)
+    table, kv = torch.zeros(1, 2, dtype=torch.int32), torch.zeros(3, 2, 64)
+    q = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
+    calls = {"attention": lambda **kw: sd2.attention_prompt(q, pool, table, 0, i(0, 3), i(3), return_lse=True, **kw),
+             "append": lambda **kw: sd2.pages_append(kv, kv, pool, table, 0, i(0, 3), i(3), **kw),
+             "fork": lambda **kw: sd2.pages_fork(pool, table, i(3), i(0), **kw),
+             "compact": lambda **kw: sd2.pages_compact(pool, table, i(1), i(1, 0, 0, 0), **kw)}
+    return calls, made, handles
+
+
+class _Stream:
+    device = None
+
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+@pytest.mark.parametrize("name,n_out,n_made", [("attention", 2, 3), ("append", 0, 0), ("fork", 4, 5), ("compact", 4, 5)])
+def test_memory_comes_from_the_stream_that_uses_it(monkeypatch, name, n_out, n_made):
+    """What a call allocates for work on a given stream is that stream's memory: a block of the caller's stream may
+    still be written by work that is pending there. The outputs are noted as used on the caller's stream."""
+    caller, side = _Stream(3), _Stream(7)
+    current = [caller]
+    calls, made, handles = _host_calls(monkeypatch, current)
+    out = calls[name](stream=side)
+    assert handles == [7] and made == [side] * n_made and current == [caller]
+    outs = list(out) if out is not None else []
+    assert len(outs) == n_out and all(t.streams == [caller] for t in outs)
+    del made[:], handles[:]
+    calls[name]()
+    assert handles == [3] and made == [caller] * n_made
+
+
+def test_a_given_workspace_is_kept_for_its_stream(monkeypatch):
+    caller, side = _Stream(3), _Stream(7)
+    calls, made, handles = _host_calls(monkeypatch, [caller])
+    ws = torch.zeros(4096, dtype=torch.uint8).as_subclass(_Recorded)
+    calls["fork"](stream=side, workspace=ws)
+    assert len(made) == 4 and ws.streams == [side]
