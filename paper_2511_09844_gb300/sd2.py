@@ -462,7 +462,10 @@ def _pool_shape(pool: torch.Tensor):
     if not (pool.is_cuda and pool.dtype == torch.bfloat16 and len(shape) == 6 and pool.is_contiguous() and
             shape[2] == 2 and shape[4] == 16):
         _refuse("pool must be a contiguous CUDA bf16 tensor [L, n_blocks, 2, Hkv, 16, hd]")
-    return shape[0], shape[1], shape[3], shape[5], pool.get_device()
+    index = pool.get_device()
+    if index != torch.cuda.current_device():   # (the library launches there)
+        _refuse("pool must be on the current device")
+    return shape[0], shape[1], shape[3], shape[5], index
 
 
 def _ints(name: str, t: Optional[torch.Tensor], shape: tuple, index: int):

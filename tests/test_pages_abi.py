@@ -209,3 +209,31 @@ def test_a_given_workspace_is_kept_for_its_stream(monkeypatch):
     ws = torch.zeros(4096, dtype=torch.uint8).as_subclass(_Recorded)
     calls["fork"](stream=side, workspace=ws)
     assert len(made) == 4 and ws.streams == [side]
+
+
+def test_binding_refuses_a_pool_on_another_device(monkeypatch):
+    """The library launches on the current device: tensors of another one are refused."""
+    class Pool:
+        is_cuda, dtype, shape, device = True, torch.bfloat16, (1, 4, 2, 2, 16, 64), torch.device("cuda", 1)
+
+        def is_contiguous(self):
+            return True
+
+        def get_device(self):
+            return 1
+
+        def data_ptr(self):
+            return 1 << 20
+
+    i = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    q, kv, table = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.zeros(3, 2, 64), torch.zeros(1, 2, dtype=torch.int32)
+    pool = Pool()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for call in (lambda: sd2.attention_prompt(q, pool, table, 0, i(0, 3), i(3)),
+                 lambda: sd2.pages_append(kv, kv, pool, table, 0, i(0, 3), i(3)),
+                 lambda: sd2.pages_fork(pool, table, i(3), i(0)),
+                 lambda: sd2.pages_compact(pool, table, i(1), i(1, 0, 0, 0))):
+        with pytest.raises(sd2.SD2Error, match="EINVAL.*current device"):
+            call()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    assert sd2._pool_shape(pool) == (1, 4, 2, 64, 1)
