@@ -379,7 +379,7 @@ sd2_status sd2_accept_logits_noalloc_check(void* stream);
  * position d_kv_len[s] - 1 (d_cu_rows [n_seq + 1] starts at 0 and does not fall). All of these are
  * device memory, read on the given stream; no call waits for the GPU or allocates device memory.
  * d_err (may be null): a device word or-ed with 2 (a wait timed out), 4 (a page id, parent or
- * position out of range: the entry is skipped) or 8 (the pool has too few free pages).
+ * position out of range; each call says what it does then) or 8 (the pool has too few free pages).
  * ------------------------------------------------------------------------------------------- */
 
 /* Causal grouped-query attention of packed prompt rows over the paged cache, the rows' own K/V
@@ -388,6 +388,7 @@ sd2_status sd2_accept_logits_noalloc_check(void* stream);
  *   d_q bf16, row m's H heads of hd at d_q + m * ldq (ldq >= H * hd, a multiple of 8); d_out bf16
  *   [M, H * hd]; d_lse f32 [M, H] or null. hd 64 or 128; H a multiple of Hkv, H / Hkv <= 128.
  * A row with p < 0 sees nothing: out 0, lse -inf. Rows at or beyond d_cu_rows[n_seq] are not written.
+ * Positions of a page id outside [0, n_blocks) are hidden from every row (d_err bit 4).
  * Positions at or beyond min(d_kv_len[s], 16 * bt_stride) are not read, whatever their page holds; an
  * infinity or NaN below it reaches the rows that see its position (in V: its column of them), no others.
  * max_kv >= every d_kv_len[s] lets the call cut long caches into splits where there are few rows (it

@@ -376,14 +376,29 @@ __device__ __forceinline__ bool read_block(uint32_t answer, int& x, int& y, int&
 // K/V tiles slot s takes: from jb (+ 1 for slot 1 of solo work) in steps of 1 (2) below
 __device__ __forceinline__ int last_tile(const Work& w, int s) { return min(w.je, (w.end[s] + kTile - 1) / kTile); }
 
-// A masked probability is 0, and 0 times an infinity or NaN in V is NaN: in a tile that some rows of a slot see further
-// than others, such a value reaches columns of rows that do not see it. One warp computes these columns again, without
-// the tensor cores, for rows `need` of its 32, four at a time (r: this lane's query vector, m and l its reference and
-// sum). Columns that the rows' own positions make NaN end early. (Inlined and fed from kept[]: looking for such columns
-// and having this at hand costs 0 to 2% of a call's time, as a function called from here 3 to 6%. One such value in a
-// prompt of 16384, 32/8 heads of 128: 13 ms instead of 1.3; one in every 128 positions, each in another column: 140 ms.)
+// Whether one of the pages that the slots of a piece see does not exist, which is reported (one warp).
+__device__ __forceinline__ bool missing_page(const PromptArgs& a, const Work& w) {
+  const int* row = a.table + static_cast<size_t>(w.seq) * a.bt_stride;
+  const int end = min(w.je * kTile, max(w.end[0], w.end[1]));
+  bool bad = false;
+  for (int i = w.jb * (kTile / kPage) + (threadIdx.x & 31); i * kPage < end; i += 32) bad |= row[i] < 0 || row[i] >= a.n_blocks;
+  if (bad) atomicOr(a.err, static_cast<unsigned>(ERR_RANGE));
+  return __any_sync(0xffffffffu, bad);
+}
+
+// What the tensor cores' way through a piece cannot give, one warp computes again without them, for rows `need` of
+// its 32, four at a time (r: this lane's query vector, m and l its reference and sum).
+//  * Columns of the results (not `whole`): a masked probability is 0, and 0 times an infinity or NaN in V is NaN: in a
+//    tile that some rows of a slot see further than others, such a value reaches columns of rows that do not see it.
+//    Columns that the rows' own positions make NaN end early.
+//  * Whole rows: those that see a page that does not exist, whose zeros took part with scores of 0. First their
+//    maximum, then the sum and every column; their statistics are written, too.
+// (Inlined and fed from kept[]: looking for such columns and having this at hand costs 0 to 2% of a call's time, as a
+// function called from here 3 to 6%. One such value of V in a prompt of 16384, 32/8 heads of 128: 13 ms instead of 1.3;
+// one in every 128 positions, each in another column: 140 ms.)
 template <int HD>
-__device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, int s, int r, unsigned need, float m, float l) {
+__device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, int s, int r, unsigned need, float m, float l,
+                                          bool whole) {
   constexpr int kPer = HD / 32, kRows = 4;
   const int lane = threadIdx.x & 31;
   const int* row = a.table + static_cast<size_t>(w.seq) * a.bt_stride;
@@ -397,9 +412,11 @@ __device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, in
   const size_t to_v = static_cast<size_t>(a.Hkv) * kPage * HD;
   struct alignas(2 * kPer) Cols { bf16 v[kPer]; };
   const int first = w.solo ? 0 : s * a.T, r0 = r - lane;
+  __syncwarp();                              // (the results and statistics so far are written)
 #pragma unroll 1
   while (need) {
-    float m_r[kRows], inv_r[kRows], acc[kRows][kPer] = {};
+    // the reference: top * scale + m, in log2
+    float top[kRows], m_r[kRows], l_r[kRows], acc[kRows][kPer] = {};
     int see_r[kRows], see_min = INT_MAX, see_max = 0;
     const bf16* q[kRows];
     size_t item[kRows];
@@ -408,8 +425,10 @@ __device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, in
     for (int k = 0; k < kRows; ++k) {        // (the last row again where there are no four)
       if (need) src = __ffs(need) - 1;
       need &= need - 1;
+      top[k] = whole ? -INFINITY : 0.f;
       m_r[k] = __shfl_sync(0xffffffffu, m, src);
-      inv_r[k] = 1.f / __shfl_sync(0xffffffffu, l, src);
+      l_r[k] = __shfl_sync(0xffffffffu, l, src);
+      if (whole) m_r[k] = l_r[k] = 0.f;
       const int t = first + (r0 + src) / a.G, head = w.hk * a.G + (r0 + src) % a.G;
       see_r[k] = min(w.pos0 + t + 1, w.kv);
       see_min = min(see_min, see_r[k]);
@@ -419,80 +438,111 @@ __device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, in
     }
     auto part = [&](int k) { return a.part_o + (static_cast<size_t>(w.split) * a.M * a.H + item[k]) * HD + lane * kPer; };
     auto out = [&](int k) { return a.out + item[k] * HD + lane * kPer; };
-    unsigned mine = 0;                       // this lane's columns with such a value at a position the row does not see
+    unsigned mine = whole ? (1u << (kRows * kPer)) - 1u : 0u;   // this lane's columns to compute
+    if (!whole) {                            // those with such a value at a position the row does not see
 #pragma unroll 1
-    for (int j = max(see_min, begin); j < end; ++j) {
-      const bf16* key = keys(j);
-      if (!key) continue;
-      const Cols v = *reinterpret_cast<const Cols*>(key + to_v + lane * kPer);
-      unsigned odd = 0;
+      for (int j = max(see_min, begin); j < end; ++j) {
+        const bf16* key = keys(j);
+        if (!key) continue;
+        const Cols v = *reinterpret_cast<const Cols*>(key + to_v + lane * kPer);
+        unsigned odd = 0;
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) odd |= (__bfloat162float(v.v[e]) * 0.f == 0.f ? 0u : 1u) << e;
+        for (int e = 0; e < kPer; ++e) odd |= (__bfloat162float(v.v[e]) * 0.f == 0.f ? 0u : 1u) << e;
+#pragma unroll
+        for (int k = 0; k < kRows; ++k)
+          if (j >= see_r[k]) mine |= odd << (k * kPer);
+      }
+      unsigned now = 0;                      // of them, those that are NaN
 #pragma unroll
       for (int k = 0; k < kRows; ++k)
-        if (j >= see_r[k]) mine |= odd << (k * kPer);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+          const float x = a.n_splits > 1 ? part(k)[e] : __bfloat162float(out(k)[e]);
+          if (x != x) now |= 1u << (k * kPer + e);
+        }
+      mine &= now;
     }
-    unsigned now = 0;                        // of them, those that are NaN
-#pragma unroll
-    for (int k = 0; k < kRows; ++k)
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        const float x = a.n_splits > 1 ? part(k)[e] : __bfloat162float(out(k)[e]);
-        if (x != x) now |= 1u << (k * kPer + e);
-      }
-    mine &= now;
     unsigned open = mine;
     const int limit = min(end, see_max);
 #pragma unroll 1
-    for (int j0 = begin; j0 < limit && __any_sync(0xffffffffu, open); j0 += 32) {
-      const int n = min(32, limit - j0);
-      const bf16* key = lane < n ? keys(j0 + lane) : nullptr;
-      float p[kRows] = {};
-      if (key) {
+    for (int phase = whole ? 0 : 1; phase < 2; ++phase) {       // the maximum, then the columns
+#pragma unroll 1
+      for (int j0 = begin; j0 < limit && __any_sync(0xffffffffu, open); j0 += 32) {
+        const int n = min(32, limit - j0);
+        const bf16* key = lane < n ? keys(j0 + lane) : nullptr;
+        float p[kRows] = {};
+        if (key) {
 #pragma unroll 2
-        for (int c = 0; c < HD; c += 8) {
-          const uint4 y = *reinterpret_cast<const uint4*>(key + c);
-          const __nv_bfloat162* y2 = reinterpret_cast<const __nv_bfloat162*>(&y);
+          for (int c = 0; c < HD; c += 8) {
+            const uint4 y = *reinterpret_cast<const uint4*>(key + c);
+            const __nv_bfloat162* y2 = reinterpret_cast<const __nv_bfloat162*>(&y);
 #pragma unroll
-          for (int k = 0; k < kRows; ++k) {
-            const uint4 x = *reinterpret_cast<const uint4*>(q[k] + c);
-            const __nv_bfloat162* x2 = reinterpret_cast<const __nv_bfloat162*>(&x);
+            for (int k = 0; k < kRows; ++k) {
+              const uint4 x = *reinterpret_cast<const uint4*>(q[k] + c);
+              const __nv_bfloat162* x2 = reinterpret_cast<const __nv_bfloat162*>(&x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 u = __bfloat1622float2(x2[e]), v = __bfloat1622float2(y2[e]);
-              p[k] = fmaf(u.x, v.x, fmaf(u.y, v.y, p[k]));
+              for (int e = 0; e < 4; ++e) {
+                const float2 u = __bfloat1622float2(x2[e]), v = __bfloat1622float2(y2[e]);
+                p[k] = fmaf(u.x, v.x, fmaf(u.y, v.y, p[k]));
+              }
             }
           }
         }
-      }
+        if (phase == 0) {
 #pragma unroll
-      for (int k = 0; k < kRows; ++k) p[k] = ex2(p[k] * scale - m_r[k]);
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) {
-        const bf16* k_i = reinterpret_cast<const bf16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(key), i));
-        Cols v = {};
-        if (k_i) v = *reinterpret_cast<const Cols*>(k_i + to_v + lane * kPer);
+          for (int k = 0; k < kRows; ++k)
+            if (key && j0 + lane < see_r[k]) top[k] = fmaxf(top[k], p[k]);
+          continue;
+        }
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
-          const float p_i = __shfl_sync(0xffffffffu, p[k], i);
-          if (j0 + i >= see_r[k]) continue;
+          p[k] = key ? ex2((p[k] - top[k]) * scale - m_r[k]) : 0.f;
+          if (whole && j0 + lane < see_r[k]) l_r[k] += p[k];
+        }
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+          const bf16* k_i = reinterpret_cast<const bf16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(key), i));
+          Cols v = {};
+          if (k_i) v = *reinterpret_cast<const Cols*>(k_i + to_v + lane * kPer);
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) acc[k][e] = fmaf(p_i, __bfloat162float(v.v[e]), acc[k][e]);
+          for (int k = 0; k < kRows; ++k) {
+            const float p_i = __shfl_sync(0xffffffffu, p[k], i);
+            if (j0 + i >= see_r[k]) continue;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) acc[k][e] = fmaf(p_i, __bfloat162float(v.v[e]), acc[k][e]);
+          }
+        }
+        if (!whole) {
+#pragma unroll
+          for (int k = 0; k < kRows; ++k)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+              if (acc[k][e] != acc[k][e]) open &= ~(1u << (k * kPer + e));
         }
       }
+      if (phase == 0) {
 #pragma unroll
-      for (int k = 0; k < kRows; ++k)
-#pragma unroll
-        for (int e = 0; e < kPer; ++e)
-          if (acc[k][e] != acc[k][e]) open &= ~(1u << (k * kPer + e));
+        for (int k = 0; k < kRows; ++k) {
+          top[k] = warp_max(top[k]);
+          if (top[k] == -INFINITY) top[k] = 0.f;                // nothing seen
+        }
+      }
     }
 #pragma unroll
-    for (int k = 0; k < kRows; ++k)
+    for (int k = 0; k < kRows; ++k) {
+      if (whole) l_r[k] = warp_sum(l_r[k]);
+      const float inv = l_r[k] == 0.f ? 0.f : 1.f / l_r[k];
 #pragma unroll
       for (int e = 0; e < kPer; ++e)
         if (mine >> (k * kPer + e) & 1) {
-          if (a.n_splits > 1) part(k)[e] = acc[k][e] * inv_r[k]; else out(k)[e] = __float2bfloat16(acc[k][e] * inv_r[k]);
+          if (a.n_splits > 1) part(k)[e] = acc[k][e] * inv; else out(k)[e] = __float2bfloat16(acc[k][e] * inv);
         }
+      if (whole && lane == 0) {
+        const float l2 = l_r[k] == 0.f ? -INFINITY : top[k] * scale + log2f(l_r[k]);
+        if (a.n_splits > 1) a.part_lse[static_cast<size_t>(w.split) * a.M * a.H + item[k]] = l2;
+        else if (a.lse) a.lse[item[k]] = l2 * 0.6931471805599453f;
+      }
+    }
   }
   __syncwarp();
 }
@@ -508,7 +558,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
   __shared__ Work works[2], kept[8];       // kept: each softmax warp's, until its results are out
   __shared__ __align__(16) uint4 answer;
   __shared__ float twin[2][kTile];         // slot 1's references and sums, for slot 0 (solo work)
-  __shared__ int flags[3];                 // [0] abort, [1] TMEM base, [2] the block has work of its own
+  __shared__ int flags[4];                 // [0] abort, [1] TMEM base, [2] the block has work of its own, [3] it has met a
+                                           // page id outside the pool
   __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 22];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * S, q_full = empty0 + 8 * S, q_empty = q_full + 8,
@@ -535,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
     if (lane < 3)
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&a.map_q + lane)) : "memory");
   } else if (threadIdx.x == 0) {
-    flags[0] = 0;
+    flags[0] = flags[3] = 0;
     for (int i = 0; i < S; ++i) {
       mbar_init(full0 + 8 * i, 1);
       mbar_init(empty0 + 8 * i, 1);
@@ -622,10 +673,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
           if (v == v_warp) {
             int np = min(kTile / kPage, n_pages - j * (kTile / kPage));
             const bool bad = page_id < 0 || page_id >= a.n_blocks;
-            if (bad && page < np && a.err) atomicOr(a.err, static_cast<unsigned>(ERR_RANGE));
+            if (bad && page < np) abort_flag[3] = 1;   // (before the tile is there: its scores come after that)
             if (!wait_warp(empty0 + 8 * st, ph ^ 1)) return false;
             const uint32_t dst = kv_smem + st * Lay::kSlotBytes;
-            // a page that does not exist lies outside the map: zeros
+            // a page that does not exist lies outside the map: zeros (rows that see it are computed again)
             const int at = bad ? a.kv_rows : ((page_id * 2 + v) * a.Hkv + w.hk) * kPage;
             const int rows = w.kv - (j * kTile + (np - 1) * kPage);   // of the last page, that exist
             if (v && ((np & 3) || rows < kPage)) {
@@ -1058,7 +1109,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       }
       const uint32_t put = panel + lane * 128, put_x = (lane & 7) * 16;
       const uint32_t get = panel + lane / 8 * 128 + ((lane % 8) ^ (lane / 8)) * 16;   // (row + 4 flips chunk bit 2)
-      uint64_t odd = 0ull;                   // 0 times every result: NaN if one is not finite
+      // 0 times every result: NaN if one is not finite (or the block has met a page that does not exist)
+      uint64_t odd = pair(abort_flag[3] ? NAN : 0.f, 0.f);
 #pragma unroll 1
       for (int c = 0; c < HD / 32; ++c) {    // (not unrolled: the code of a rare path is fetched each time)
         uint32_t o[32];
@@ -1101,8 +1153,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       }
       float odd0, odd1;
       unpair(odd, odd0, odd1);
-      if (const unsigned need = __ballot_sync(0xffffffffu, valid && !(odd0 + odd1 == 0.f) && l - l == 0.f))
-        mend_rows<HD>(a, kept[warp], s, r, need, m, l);
+      // all of each row where the piece sees a page that does not exist, else the columns that are not finite
+      if (__any_sync(0xffffffffu, !(odd0 + odd1 == 0.f))) {
+        const bool whole = abort_flag[3] && missing_page(a, kept[warp]);
+        const unsigned need = __ballot_sync(0xffffffffu, valid && (whole || (!(odd0 + odd1 == 0.f) && l - l == 0.f)));
+        mend_rows<HD>(a, kept[warp], s, r, need, m, l, whole);
+      }
     }
   }
   tc_fence_before();

@@ -500,3 +500,66 @@ def test_a_block_freed_behind_pending_work_is_not_taken_on_another_stream():
                                     return_lse=True, stream=side)
         torch.cuda.synchronize()
         assert torch.equal(o.cpu(), out) and torch.equal(l.cpu(), lse)
+
+
+def _without(c, bad):
+    """_definition with the positions of the pages `bad` (sequence, index in its table row) hidden from every row."""
+    H, Hkv, hd = c["H"], c["Hkv"], c["hd"]
+    M = c["q"].shape[0]
+    out, mag = torch.zeros(M, H, hd, dtype=torch.float64), torch.zeros(M, H, hd, dtype=torch.float64)
+    lse = torch.full((M, H), float("-inf"), dtype=torch.float64)
+    for s, (n, L) in enumerate(zip(c["rows"], c["kv"])):
+        kv = c["pool"][c["layer"], c["table"][s, : (L + 15) // 16].long()].double()
+        k = kv[:, 0].transpose(0, 1).reshape(Hkv, -1, hd)[:, :L].repeat_interleave(H // Hkv, 0)
+        v = kv[:, 1].transpose(0, 1).reshape(Hkv, -1, hd)[:, :L].repeat_interleave(H // Hkv, 0)
+        r0, at = int(c["cu"][s]), torch.arange(L)
+        hidden = at[None, :] > torch.arange(L - n, L)[:, None]
+        for b, i in bad:
+            if b == s:
+                hidden |= at[None, :] // 16 == i
+        seen = ~hidden.all(1)
+        z = torch.einsum("rhd,hkd->hrk", c["q"][r0:r0 + n].double(), k) / hd ** 0.5
+        z = z.masked_fill(hidden, float("-inf"))[:, seen]
+        lse[r0:r0 + n][seen] = torch.logsumexp(z, -1).T
+        w = torch.softmax(z, -1)
+        out[r0:r0 + n][seen] = torch.einsum("hrk,hkd->rhd", w, v)
+        mag[r0:r0 + n][seen] = torch.einsum("hrk,hkd->rhd", w, v.abs())
+    return out.reshape(M, -1), lse, mag.reshape(M, -1)
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(8, 2, 128), (14, 2, 64), (3, 1, 128), (4, 4, 64)])
+@pytest.mark.parametrize("rows,kv,bad", [
+    ([300, 5], [300, 300], [(0, 0), (1, 18)]),                                   # the first page, a partial last page
+    ([40, 7], [777, 1000], [(0, i) for i in range(8, 16)] + [(0, 20), (1, 62)]),   # a whole K/V tile
+    ([1, 2], [5000, 3000], [(0, 100), (0, 312)] + [(1, i) for i in range(64)]),    # split positions
+    ([3, 20], [40, 200], [(0, i) for i in range(3)] + [(1, 5)]),                   # nothing left to see
+    ([700, 9, 130], [700, 400, 130], [(0, 1), (0, 2), (0, 43)])])                # clean pieces after others
+def test_positions_of_bad_pages_are_hidden(rows, kv, bad, H, Hkv, hd):
+    """A page id outside the pool is reported, and its positions weigh nothing: not as zeros, which would count in
+    every sum."""
+    c = _case(rows, kv, H, Hkv, hd, seed=len(bad) + hd)
+    want = _without(c, bad)
+    t = dict(c, table=c["table"].clone())
+    for n, (s, i) in enumerate(bad):
+        t["table"][s, i] = (-1, c["pool"].shape[1], 2 ** 31 - 1, -2 ** 31)[n % 4]
+    out, lse, err = _run(t)
+    assert err == ERR_RANGE
+    _check(c, out, lse, want)
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(8, 2, 128), (14, 2, 64)])
+def test_bad_pages_beside_values_that_only_later_rows_see(H, Hkv, hd):
+    c = _case([60], [200], H, Hkv, hd, seed=23)
+    bad = [(0, 2), (0, 9)]
+    o, l, mag = _without(c, bad)
+    c["pool"][c["layer"], int(c["table"][0, 11]), 1, 0, 7, 5] = float("nan")        # position 183: rows from 43 on
+    t = dict(c, table=c["table"].clone())
+    t["table"][0, 2], t["table"][0, 9] = -1, c["pool"].shape[1]
+    out, lse, err = _run(t)
+    assert err == ERR_RANGE
+    spoilt = torch.zeros(60, H, hd, dtype=torch.bool)
+    spoilt[43:, : H // Hkv, 5] = True
+    spoilt = spoilt.view(60, -1)
+    assert torch.isnan(out[spoilt].float()).all() and torch.isfinite(out[~spoilt].float()).all()
+    assert ((out.double() - o).abs() - _bound(o, mag))[~spoilt].max().item() <= 1e-6
+    assert (lse.double() - l).abs().max().item() <= LSE_TOL
