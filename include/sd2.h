@@ -406,7 +406,8 @@ sd2_status sd2_attention_prompt(const void* d_q, int64_t ldq, int32_t M, int32_t
 
 /* Write packed K and V rows (rotary embedding applied by the caller) to their pages of `layer`:
  * row m's Hkv heads of hd are at d_k + m * ldk and d_v + m * ldv, f32 (rounded to the nearest bf16) or
- * bf16, 16-byte aligned rows. A row whose position lies outside [0, 16 * bt_stride) is skipped. The
+ * bf16, 16-byte aligned rows. A row whose position lies outside [0, 16 * bt_stride), or whose
+ * page id lies outside [0, n_blocks), is skipped (d_err bit 4). The
  * pages written must belong to one sequence alone (sd2_pages_fork sees to it). hd a multiple of 8. */
 sd2_status sd2_pages_append(const void* d_k, int64_t ldk, const void* d_v, int64_t ldv, int32_t dtype, int32_t M,
                             int32_t Hkv, int32_t hd, void* d_pool, int32_t n_blocks, const int32_t* d_table,
@@ -425,6 +426,9 @@ sd2_status sd2_pages_append(const void* d_k, int64_t ldk, const void* d_v, int64
  *   [n_blocks] (holders of each page, pinned ones included; 0: free).
  * New pages are the lowest free ids, granted in the order of b. When they run out (d_err bit 8) a
  * sequence without a page for its tail is cut to its whole pages, and the room ends with d_pages_out.
+ * A page id outside [0, n_blocks) (d_err bit 4): a whole page becomes page 0, which the sequence then holds
+ * like any other (its positions are page 0's); a partial last page is dropped, the sequence cut to its
+ * whole pages. A parent at or beyond n_seq counts as none (bit 4).
  * d_workspace: sd2_pages_fork_workspace_bytes(n_out, n_blocks) bytes, 256-byte aligned, contents need
  * not be initialised. n_out * bt_stride below 2^31, bt_stride at most 2^26. Work that still reads the
  * freed pages must come before this call on its stream. */
@@ -439,6 +443,8 @@ sd2_status sd2_pages_fork(void* d_pool, int32_t L, int32_t n_blocks, int32_t Hkv
  * takes the j-th lowest live page at or above it, the others stay. d_pages [n_seq]: entries in use of
  * each table row. Outputs: d_table_out (entries renamed, unused ones 0; may be d_table), d_ref_out
  * (not d_ref), d_map [n_blocks] (a page's new id, -1 for a free one), d_n_live [1] = N.
+ * An entry in use that names no live page becomes 0 (d_err bit 4): what it stood for is lost, and page 0 may be
+ * another sequence's, so that such a sequence must not be appended to.
  * d_workspace: sd2_pages_compact_workspace_bytes(n_blocks) bytes, 256-byte aligned, contents need not
  * be initialised. */
 size_t sd2_pages_compact_workspace_bytes(int32_t n_blocks);

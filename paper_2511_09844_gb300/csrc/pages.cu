@@ -176,12 +176,11 @@ __device__ __forceinline__ void fork_count(const ForkArgs& a, const ForkSeq& s, 
     int p = 0;
     if (i < full) {
       p = a.table[static_cast<size_t>(s.parent) * a.stride + i];
-      if (p >= 0 && p < a.n_blocks) {
-        atomicAdd(&count[p], 1);
-      } else {
+      if (p < 0 || p >= a.n_blocks) {      // page 0 takes its place, held like any other: nobody may write to it
         p = 0;
         raise(a.err, ERR_RANGE);
       }
+      atomicAdd(&count[p], 1);
     }
     out[i] = p;
   }
@@ -202,7 +201,8 @@ __device__ __forceinline__ void fork_grant(const ForkArgs& a, const ForkSeq& s, 
   int* out = a.table_out + static_cast<size_t>(b) * a.stride;
   const bool copied = s.tail() && kept == s.full();
   if (lane == 0) {
-    a.len_out[b] = copied && !n ? s.full() * kPage : s.keep;   // no page for the tail: cut to the whole pages
+    // no page for the tail, or none that it could come from: cut to the whole pages
+    a.len_out[b] = copied && (!n || s.last < 0) ? s.full() * kPage : s.keep;
     a.pages_out[b] = kept + n;
     if (kept > s.full()) out[s.full()] = s.last;
   }

@@ -386,3 +386,30 @@ def test_fork_at_the_limit_of_default_shared_memory():
     for size, p in zip(sizes, procs):
         out, _ = p.communicate(timeout=300)
         assert p.returncode == 0, (size, out)
+
+
+@pytest.mark.parametrize("n_blocks", [8, 13000])
+def test_fork_of_bad_page_ids_shares_no_page_unawares(n_blocks):
+    """A whole page out of range becomes page 0, held and counted like any other: it is not granted, and its owner may
+    not append to it. A partial last page out of range is dropped: its sequence is cut to its whole pages."""
+    pool = _pool(2, n_blocks, 1, 8)
+    before, err = pool.clone(), _i([0])
+    # sequence 2 ends inside page 0; its child 2 would keep it as its own if nobody else held it
+    f = sd2.pages_fork(pool, _i([[3, n_blocks, 2, 0], [5, -4, 0, 0], [7, 0, 0, 0]]), _i([40, 20, 25]), _i([0, 1, 2]),
+                       grow=_i([16, 0, 0]), err=err)
+    assert int(err) == ERR_RANGE
+    assert f.table.tolist() == [[3, 0, 2, 1], [5, 4, 0, 0], [7, 6, 0, 0]]
+    assert f.length.tolist() == [40, 16, 25] and f.pages.tolist() == [4, 2, 2]
+    assert f.ref.tolist() == [1] * 8 + [0] * (n_blocks - 8)
+    want = before.clone()
+    want[:, 6, :, :, :9] = before[:, 0, :, :, :9]
+    assert torch.equal(_bits(pool), _bits(want))
+    # a row more for each: nothing of it lands in page 0
+    rows, err = torch.ones(3, 1, 8, device="cuda"), _i([0])
+    sd2.pages_append(rows, rows, pool, f.table, 0, _i([0, 1, 2, 3]), f.length + 1, err=err)
+    for page, row in ((2, 8), (4, 0), (6, 9)):
+        want[0, page, :, :, row] = 1.0
+    assert int(err) == 0 and torch.equal(_bits(pool), _bits(want))
+    # and in the next generation page 0 is shared, not somebody's own
+    g = sd2.pages_fork(pool, f.table, f.length, _i([0, 2]), err=err)
+    assert int(err) == 0 and g.table.tolist() == [[3, 0, 2, 0], [7, 6, 0, 0]] and g.ref.tolist()[:8] == [1, 0, 1, 1, 0, 0, 1, 1]
