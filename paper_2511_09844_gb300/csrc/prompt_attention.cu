@@ -65,7 +65,10 @@ constexpr float kGrowth = 8.f;             // log2 of the growth of a maximum th
 // of 128: 31.7 us from 3 on, 34.2 from 4 on; one row on 1000 positions: 11.7 us from 2 on, 11.4 from 3, 11.3 from 4)
 constexpr int kSoloTiles = 3;
 constexpr float kSumGrowth = 4096.f;       // and the sum of a tile's 128 probabilities that shows it (heads of 64)
-constexpr float kNone = -1e30f;            // the reference before a row has seen anything
+constexpr float kNone = -1e38f;            // the reference before a row has seen anything (below every finite score in log2)
+// A reference beyond 2^16 (scores beyond 45000) is rounded by 2^-8 and more when it is scaled, or joined with a sum: such
+// rows are computed again from their scores' differences.
+constexpr float kFar = 65536.f;
 
 struct PromptArgs {
   CUtensorMap map_q, map_k, map_v;
@@ -79,6 +82,7 @@ struct PromptArgs {
   bf16* out;
   float* lse;
   float *part_o, *part_lse;                // [n_splits][M * H][hd] and [n_splits][M * H] (log2)
+  float2* part_far;                        // [n_splits][M * H], where |part_lse| > kFar: largest score, log2 of the sum
   unsigned* err;
 };
 
@@ -391,11 +395,13 @@ __device__ __forceinline__ bool missing_page(const PromptArgs& a, const Work& w)
 //  * Columns of the results (not `whole`): a masked probability is 0, and 0 times an infinity or NaN in V is NaN: in a
 //    tile that some rows of a slot see further than others, such a value reaches columns of rows that do not see it.
 //    Columns that the rows' own positions make NaN end early.
-//  * Whole rows: those that see a page that does not exist, whose zeros took part with scores of 0. First their
-//    maximum, then the sum and every column; their statistics are written, too.
+//  * Whole rows: those that see a page that does not exist, whose zeros took part with scores of 0, and those with
+//    scores beyond kFar. First their maximum, then the sum and every column; their statistics are written, too.
 // (Inlined and fed from kept[]: looking for such columns and having this at hand costs 0 to 2% of a call's time, as a
 // function called from here 3 to 6%. One such value of V in a prompt of 16384, 32/8 heads of 128: 13 ms instead of 1.3;
-// one in every 128 positions, each in another column: 140 ms.)
+// one in every 128 positions, each in another column: 140 ms. Whole rows, a prompt of 4096: 23 to 25 ms instead of 0.12;
+// a piece takes some 3.3 us per position, so that beyond half a million positions the other warps' waits give up, with
+// ERR_TIMEOUT.)
 template <int HD>
 __device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, int s, int r, unsigned need, float m, float l,
                                           bool whole) {
@@ -462,7 +468,7 @@ __device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, in
         }
       mine &= now;
     }
-    unsigned open = mine;
+    unsigned open = mine, nan = 0;
     const int limit = min(end, see_max);
 #pragma unroll 1
     for (int phase = whole ? 0 : 1; phase < 2; ++phase) {       // the maximum, then the columns
@@ -491,7 +497,12 @@ __device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, in
         if (phase == 0) {
 #pragma unroll
           for (int k = 0; k < kRows; ++k)
-            if (key && j0 + lane < see_r[k]) top[k] = fmaxf(top[k], p[k]);
+            if (key && j0 + lane < see_r[k]) {
+              top[k] = fmaxf(top[k], p[k]);
+              nan |= (p[k] != p[k] ? 1u : 0u) << k;
+            }
+          nan = __reduce_or_sync(0xffffffffu, nan);
+          if (nan == (1u << kRows) - 1u) break;
           continue;
         }
 #pragma unroll
@@ -525,6 +536,12 @@ __device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, in
         for (int k = 0; k < kRows; ++k) {
           top[k] = warp_max(top[k]);
           if (top[k] == -INFINITY) top[k] = 0.f;                // nothing seen
+          if (nan >> k & 1) {                                   // settled
+            top[k] = l_r[k] = NAN;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) acc[k][e] = NAN;
+            open &= ~(((1u << kPer) - 1u) << (k * kPer));
+          }
         }
       }
     }
@@ -538,9 +555,14 @@ __device__ __forceinline__ void mend_rows(const PromptArgs& a, const Work& w, in
           if (a.n_splits > 1) part(k)[e] = acc[k][e] * inv; else out(k)[e] = __float2bfloat16(acc[k][e] * inv);
         }
       if (whole && lane == 0) {
-        const float l2 = l_r[k] == 0.f ? -INFINITY : top[k] * scale + log2f(l_r[k]);
-        if (a.n_splits > 1) a.part_lse[static_cast<size_t>(w.split) * a.M * a.H + item[k]] = l2;
-        else if (a.lse) a.lse[item[k]] = l2 * 0.6931471805599453f;
+        const float sum = log2f(l_r[k]), l2 = l_r[k] == 0.f ? -INFINITY : top[k] * scale + sum;
+        const size_t at = static_cast<size_t>(w.split) * a.M * a.H + item[k];
+        if (a.n_splits > 1) {
+          a.part_lse[at] = l2;
+          a.part_far[at] = make_float2(top[k], sum);
+        } else if (a.lse) {
+          a.lse[item[k]] = l2 * 0.6931471805599453f;
+        }
       }
     }
   }
@@ -1109,8 +1131,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       }
       const uint32_t put = panel + lane * 128, put_x = (lane & 7) * 16;
       const uint32_t get = panel + lane / 8 * 128 + ((lane % 8) ^ (lane / 8)) * 16;   // (row + 4 flips chunk bit 2)
-      // 0 times every result: NaN if one is not finite (or the block has met a page that does not exist)
-      uint64_t odd = pair(abort_flag[3] ? NAN : 0.f, 0.f);
+      // 0 times every result: NaN if one is not finite (or the scores are far, or the block has met a page that does not
+      // exist)
+      const bool far = fabsf(m) > kFar && m != kNone;
+      uint64_t odd = pair(far || abort_flag[3] ? NAN : 0.f, 0.f);
 #pragma unroll 1
       for (int c = 0; c < HD / 32; ++c) {    // (not unrolled: the code of a rare path is fetched each time)
         uint32_t o[32];
@@ -1148,16 +1172,20 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
       }
       if (valid) {
         const float l2 = none ? -INFINITY : m + log2f(l);
-        if (to_parts) a.part_lse[part0 + item] = l2;
+        // (only a row that is computed again below gets beyond kFar, or is a NaN)
+        if (to_parts) a.part_lse[part0 + item] = none ? l2 : fminf(fmaxf(l2, -kFar), kFar);
         else if (a.lse) a.lse[item] = l2 * 0.6931471805599453f;
       }
       float odd0, odd1;
       unpair(odd, odd0, odd1);
-      // all of each row where the piece sees a page that does not exist, else the columns that are not finite
       if (__any_sync(0xffffffffu, !(odd0 + odd1 == 0.f))) {
-        const bool whole = abort_flag[3] && missing_page(a, kept[warp]);
-        const unsigned need = __ballot_sync(0xffffffffu, valid && (whole || (!(odd0 + odd1 == 0.f) && l - l == 0.f)));
-        mend_rows<HD>(a, kept[warp], s, r, need, m, l, whole);
+        // all of a row where the piece sees a page that does not exist, its scores are far or its sum is not finite (a NaN
+        // among them, or infinities of an earlier far reference); else the columns that are not finite
+        const bool missing = abort_flag[3] && missing_page(a, kept[warp]);
+        const bool again = valid && (missing || far || l - l != 0.f), columns = valid && !again && !(odd0 + odd1 == 0.f);
+        const unsigned rows[2] = {__ballot_sync(0xffffffffu, columns), __ballot_sync(0xffffffffu, again)};
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) mend_rows<HD>(a, kept[warp], s, r, k ? rows[1] : rows[0], m, l, k != 0);
       }
     }
   }
@@ -1168,7 +1196,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attention_kernel(const __g
 }
 
 // Joins the partial results of each (row, head): o = sum_z w_z o_z / sum_z w_z, w_z = 2^{lse_z - max}. W warps
-// per item, each taking every W-th partial result, eight loads in flight.
+// per item, each taking every W-th partial result, eight loads in flight. Beyond kFar the weights come from the largest
+// scores and the sums apart.
 template <int HD, int W>
 __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant__ PromptArgs a) {
   constexpr int kPer = HD / 32, kAhead = 8;
@@ -1202,6 +1231,33 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant_
       for (int e = 0; e < kPer; ++e) acc[e] += w[i] * o[i].v[e];
     }
   }
+  float lse_max = mx;
+  if (fabsf(base) > kFar) {                  // anew (after the loop above, whose loads need not wait for this)
+    const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD));
+    auto is_far = [](float lse) { return fabsf(lse) > kFar && fabsf(lse) < INFINITY; };
+    float top = -INFINITY;                   // the largest score
+    for (int z = lane; z < parts; z += 32)
+      if (is_far(a.part_lse[z * n + item])) top = fmaxf(top, a.part_far[z * n + item].x);
+    top = warp_max(top);
+    lse_max = top * scale;
+    total = 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) acc[e] = 0.f;
+#pragma unroll 1
+    for (int z = sub; z < parts; z += W) {
+      const float lse = a.part_lse[z * n + item];
+      float w = lse - lse == 0.f ? 0.f : ex2(lse - base);   // (a NaN, and a part that saw nothing)
+      if (is_far(lse)) {
+        const float2 st = a.part_far[z * n + item];
+        w = ex2((st.x - top) * scale + st.y);
+      }
+      total += w;
+      if (w == 0.f) continue;
+      const Vec o = *reinterpret_cast<const Vec*>(a.part_o + (z * n + item) * HD + lane * kPer);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[e] += w * o.v[e];
+    }
+  }
   if (W > 1) {
 #pragma unroll
     for (int e = 0; e < kPer; ++e) acc_s[warp][lane * kPer + e] = acc[e];
@@ -1221,7 +1277,7 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const __grid_constant_
 #pragma unroll
   for (int i = 0; i < kPer; i += 2) out.v[i / 2] = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
   *reinterpret_cast<Out*>(a.out + item * HD + lane * kPer) = out;
-  if (a.lse && lane == 0) a.lse[item] = total == 0.f ? -INFINITY : (mx + log2f(total)) * 0.6931471805599453f;
+  if (a.lse && lane == 0) a.lse[item] = total == 0.f ? -INFINITY : (lse_max + log2f(total)) * 0.6931471805599453f;
 }
 
 // The grid: query tiles (an upper bound: the sequences' lengths are on the device), and splits of the
@@ -1262,7 +1318,7 @@ cudaError_t launch(const PromptArgs& a, int tiles, cudaStream_t st) {
 
 size_t prompt_attention_work_bytes(int M, int n_seq, int H, int Hkv, int hd, int max_kv) {
   const int splits = shape_of(M, n_seq, H, Hkv, hd, max_kv).splits;
-  return splits > 1 ? static_cast<size_t>(splits) * M * H * (hd + 1) * 4 : 0;
+  return splits > 1 ? static_cast<size_t>(splits) * M * H * (hd + 3) * 4 : 0;
 }
 
 cudaError_t prompt_attention(const PromptAttnArgs& p, cudaStream_t st) {
@@ -1275,7 +1331,9 @@ cudaError_t prompt_attention(const PromptAttnArgs& p, cudaStream_t st) {
   a.table = p.kv.table; a.cu = p.cu; a.kv_len = p.kv_len; a.out = static_cast<bf16*>(p.out); a.lse = p.lse; a.err = p.err;
   a.q = static_cast<const bf16*>(p.q); a.ldq = p.ldq;
   a.part_o = static_cast<float*>(p.work);
-  a.part_lse = a.part_o + static_cast<size_t>(a.n_splits) * p.M * p.H * hd;
+  const size_t parts = static_cast<size_t>(a.n_splits) * p.M * p.H;
+  a.part_far = reinterpret_cast<float2*>(a.part_o + parts * hd);
+  a.part_lse = reinterpret_cast<float*>(a.part_far + parts);
   a.pool = static_cast<const bf16*>(p.kv.pool) + static_cast<size_t>(p.layer) * p.kv.n_blocks * 2 * Hkv * kPage * hd;
   // Q: [row][head][hd], boxes of T rows x G heads x 64; K: [page row][hd], a page x 64; V: a page x all of hd,
   // one 64-column half behind the other

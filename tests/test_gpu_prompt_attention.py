@@ -563,3 +563,44 @@ def test_bad_pages_beside_values_that_only_later_rows_see(H, Hkv, hd):
     assert torch.isnan(out[spoilt].float()).all() and torch.isfinite(out[~spoilt].float()).all()
     assert ((out.double() - o).abs() - _bound(o, mag))[~spoilt].max().item() <= 1e-6
     assert (lse.double() - l).abs().max().item() <= LSE_TOL
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(8, 2, 128), (14, 2, 64)])
+@pytest.mark.parametrize("rows,prefix", [([1], [0]), ([130], [0]), ([20], [300]), ([1, 3], [3000, 0]), ([300], [500])])
+@pytest.mark.parametrize("size", [-3e35, -2e30, -1e12, 1e6, 1e12, 2e37])
+def test_scores_of_any_size(size, rows, prefix, H, Hkv, hd):
+    """Scores far beyond what an exponent holds, all of a row's alike: its result is the mean of what it sees, its
+    log-sum-exp that score."""
+    c = _case(rows, [a + b for a, b in zip(rows, prefix)], H, Hkv, hd, seed=31)
+    g = torch.Generator().manual_seed(32)
+    part = abs(size) * hd ** 0.5 / hd
+    base = (torch.rand(hd, generator=g) + 1) * part ** 0.5
+    c["q"][:] = base.to(torch.bfloat16)
+    key = (part / base * (1 if size > 0 else -1)).to(torch.bfloat16)
+    nan = torch.isnan(c["pool"][:, :, 0])
+    c["pool"][:, :, 0] = torch.where(nan, c["pool"][:, :, 0], key)
+    out, lse, err = _run(c)
+    o, l, mag = _definition(c)
+    assert err == 0
+    assert ((out.double() - o).abs() - _bound(o, mag)).max().item() <= 1e-6
+    # hd products and sums in 32 bits, each within 2^-23, and the factor's and the result's roundings
+    assert ((lse.double() - l).abs() <= (hd + 4) * 2.0 ** -23 * l.abs() + LSE_TOL).all()
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(8, 2, 128), (14, 2, 64)])
+@pytest.mark.parametrize("rows,kv", [([1], [300]), ([50], [400]), ([2], [4000])])
+@pytest.mark.parametrize("low,high", [(-3e35, -1e30), (-1e33, 2.0), (3.0, 1e15), (1e12, 1e36)])
+def test_far_scores_after_others(low, high, rows, kv, H, Hkv, hd):
+    """Positions of one far score and, later, some of a higher one: from the first of these on a row is their mean."""
+    c = _case(rows, kv, H, Hkv, hd, seed=33)
+    layer, L, n = c["layer"], kv[0], rows[0]
+    c["q"][:] = 2.0 ** 40
+    key = lambda z: z * hd ** 0.5 / hd / 2.0 ** 40  # noqa: E731
+    tops = [L - n, L - n - 130, L - n // 2 - 1]
+    for j in range(L):
+        c["pool"][layer, int(c["table"][0, j // 16]), 0, :, j % 16] = key(high if j in tops else low)
+    out, lse, err = _run(c)
+    o, l, mag = _definition(c)
+    assert err == 0
+    assert ((out.double() - o).abs() - _bound(o, mag)).max().item() <= 1e-6
+    assert ((lse.double() - l).abs() <= (hd + 4) * 2.0 ** -23 * l.abs() + LSE_TOL).all()
