@@ -604,3 +604,29 @@ def test_far_scores_after_others(low, high, rows, kv, H, Hkv, hd):
     assert err == 0
     assert ((out.double() - o).abs() - _bound(o, mag)).max().item() <= 1e-6
     assert ((lse.double() - l).abs() <= (hd + 4) * 2.0 ** -23 * l.abs() + LSE_TOL).all()
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(32, 8, 128), (32, 8, 64), (14, 2, 64)])
+def test_long_prompts_of_many_pieces(H, Hkv, hd):
+    """Several pieces of many K/V tiles per block, one after another through the same ring and barriers: chosen rows
+    against the definition, every row finite."""
+    rows, prefix = [4001, 257, 3000, 3], [0, 1500, 129, 0]
+    kv = [a + b for a, b in zip(rows, prefix)]
+    c = _case(rows, kv, H, Hkv, hd, seed=hd + H)
+    out, lse, err = _run(c)
+    assert err == 0 and torch.isfinite(out.float()).all() and torch.isfinite(lse).all()
+    g = torch.Generator().manual_seed(5)
+    for s, (n, p) in enumerate(zip(rows, prefix)):
+        at = sorted({0, n - 1, min(127, n - 1), min(128, n - 1)} | set(torch.randint(0, n, (24,), generator=g).tolist()))
+        data = c["pool"][c["layer"], c["table"][s, : (kv[s] + 15) // 16].long()].double()
+        k = data[:, 0].transpose(0, 1).reshape(Hkv, -1, hd)[:, : kv[s]]
+        v = data[:, 1].transpose(0, 1).reshape(Hkv, -1, hd)[:, : kv[s]]
+        for i in at:
+            m, seen = int(c["cu"][s]) + i, p + i + 1
+            x = c["q"][m].double().view(Hkv, H // Hkv, hd)
+            z = torch.einsum("hgd,hkd->hgk", x, k[:, :seen]) / hd ** 0.5
+            w = torch.softmax(z, -1)
+            o = torch.einsum("hgk,hkd->hgd", w, v[:, :seen]).reshape(-1)
+            mag = torch.einsum("hgk,hkd->hgd", w, v[:, :seen].abs()).reshape(-1)
+            assert ((out[m].double() - o).abs() - _bound(o, mag)).max().item() <= 1e-6
+            assert (lse[m].double() - torch.logsumexp(z, -1).reshape(-1)).abs().max().item() <= LSE_TOL
