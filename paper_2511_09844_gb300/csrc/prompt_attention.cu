@@ -34,10 +34,11 @@
 // piece with queries for one slot only puts both slots on them, with alternate K/V tiles, and joins the two at its end
 // (slot 0's threads read slot 1's columns).
 //
-// Measured (GB300, 1913 TFLOP/s bf16 and 6.77 TB/s copy): one prompt of 16384, 32/8 heads of 128, 1.19-1.26 ms,
-// 1.75-1.85 PFLOP/s; four chunks of 411-777 rows on 3K-16K positions, 40/8 heads of 128, 459-465 us, 1.71 PFLOP/s; one
-// prompt of 16384, 32/8 heads of 64, 0.935 ms, 1.18 PFLOP/s; 6 and 17 rows on 60K and 65K positions, 95-97 us,
-// 5.5 TB/s; 512 rows, 32/8 heads of 128, 13 us; 37 rows 6.3 us.
+// Measured (GB300, 1913 TFLOP/s bf16 in a burst, 1716 sustained, 6.77 TB/s copy), replayed from a graph and, in
+// brackets, as calls in a row: one prompt of 16384, 32/8 heads of 128, 1.19-1.30 ms, 1.69-1.85 PFLOP/s (1.33 ms, 1.65);
+// four chunks of 411-777 rows on 3K-16K positions, 40/8 heads of 128, 460-530 us (527 us, 1.50 PFLOP/s); one prompt of
+// 16384, 32/8 heads of 64, 0.94 ms, 1.17 PFLOP/s; 6 and 17 rows on 60K and 65K positions, 95-100 us, 5.5 TB/s (97 us); 512
+// rows, 32/8 heads of 128, 13 us; 37 rows 6.4 us.
 #include "sd2.h"
 #include "kernels.h"
 #include "tc.cuh"

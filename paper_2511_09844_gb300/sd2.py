@@ -553,7 +553,8 @@ def attention_prompt(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, l
     [M, H, hd] (any row stride); pool bf16 [L, n_blocks, 2, Hkv, 16, hd]; table int32 [n_seq, bt_stride];
     cu_rows int32 [n_seq + 1]; kv_len int32 [n_seq], the cached length with the new rows; max_kv a host
     bound of it (default: the table's room). Returns bf16 [M, H * hd], with f32 [M, H] log-sum-exps if
-    `return_lse`. Rows of no sequence are left unwritten."""
+    `return_lse`. Rows of no sequence are left unwritten. A given `stream` is made current for the call, as in the
+    calls below: what it allocates is that stream's."""
     if stream is not None:
         return _within(stream, workspace, attention_prompt, q, pool, table, layer, cu_rows, kv_len, max_kv, return_lse,
                        workspace, err)
