@@ -630,3 +630,27 @@ def test_long_prompts_of_many_pieces(H, Hkv, hd):
             mag = torch.einsum("hgk,hkd->hgd", w, v[:, :seen].abs()).reshape(-1)
             assert ((out[m].double() - o).abs() - _bound(o, mag)).max().item() <= 1e-6
             assert (lse[m].double() - torch.logsumexp(z, -1).reshape(-1)).abs().max().item() <= LSE_TOL
+
+
+@pytest.mark.parametrize("low,high", [(45425.5, 45426.5), (45426.5, 45425.5), (-45426.5, -45425.5), (45424.0, 45425.0)])
+@pytest.mark.parametrize("kv", [300, 3000])
+def test_scores_around_the_limit_of_plain_statistics(low, high, kv):
+    """Positions a factor e apart, in the same tile and in splits, on either side of where statistics are kept apart
+    (2^16 in log2). There a statistic's rounding is 2^-8 in log2: two of them are worth 2^-7 in a weight."""
+    c = _case([1], [kv], 2, 1, 64, seed=41)
+    c["q"][:] = 0.0
+    c["q"][:, :, :2] = 1.0
+    for j in range(kv):
+        page, at = int(c["table"][0, j // 16]), j % 16
+        z = 8 * (low if j < kv // 2 else high)
+        big = 362496.0 if z > 0 else -362496.0
+        c["pool"][c["layer"], page, 0, :, at] = 0.0
+        c["pool"][c["layer"], page, 0, :, at, 0] = big
+        c["pool"][c["layer"], page, 0, :, at, 1] = z - big
+        c["pool"][c["layer"], page, 1, :, at] = 1.0 if j < kv // 2 else -1.0
+    out, lse, err = _run(c)
+    o, l, mag = _definition(c)
+    assert err == 0
+    assert abs(o).max() < 0.6                          # (both levels weigh)
+    assert ((out.double() - o).abs() - _bound(o, mag) - 2 ** -7 * mag).max().item() <= 1e-6
+    assert ((lse.double() - l).abs() <= 68 * 2.0 ** -23 * l.abs() + LSE_TOL).all()
