@@ -284,11 +284,10 @@ __global__ void __launch_bounds__(kJoinThreads) quantized_join_kernel(const __gr
     r.x *= f; r.y *= f; r.z *= f; r.w *= f;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const float w = st[k].y == 0.f ? 0.f : st[k].y * ex2((st[k].x - top) * scale);
+      if (st[k].y == 0.f) continue;        // (it saw nothing)
+      const float w = st[k].y * ex2((st[k].x - top) * scale);   // (a NaN times a weight of 0 is passed on)
       total += w;
-      if (w != 0.f) {
-        r.x += w * o[k].x; r.y += w * o[k].y; r.z += w * o[k].z; r.w += w * o[k].w;
-      }
+      r.x += w * o[k].x; r.y += w * o[k].y; r.z += w * o[k].z; r.w += w * o[k].w;
     }
   }
   const float inv = total == 0.f ? 0.f : 1.f / total;
