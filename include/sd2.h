@@ -483,7 +483,9 @@ sd2_status sd2_pages_append_quantized(const void* d_k, int64_t ldk, const void* 
                                       const int32_t* d_kv_len, int32_t n_seq, uint32_t* d_err, void* stream);
 
 /* sd2_attention_prompt over the 8-bit cache, of prompts as of single tokens; through a window as in sd2_attention_window
- * if window is not 0. A NaN of the cache reaches the rows that see its position, no others. d_workspace:
+ * if window is not 0. A NaN of the cache reaches the rows that see its position, no others. Of few rows, scores may lie
+ * anywhere, also beyond fp32 (lse is infinite there); of prompts, q . k has to lie in fp32, with elements of q above 2^-110 (a row's
+ * largest beyond it gives NaN). d_workspace:
  * sd2_attention_quantized_workspace_bytes(..) bytes, else as there; for prompts this includes a bf16 copy of the layer's
  * pages, as long as that is at most 4 GB. */
 size_t sd2_attention_quantized_workspace_bytes(int32_t M, int32_t n_seq, int32_t H, int32_t Hkv, int32_t hd,

@@ -13,8 +13,8 @@
 // probabilities before they are rounded.
 //
 // 8 bits: queries are exact in f16, too, but for elements 2^-14 below their vector's largest (rounded to 2^-25 of it, as fp32
-// sums are): a vector is multiplied by the power of two that brings its largest element to 1 .. 2. Scores stay unscaled in
-// fp32 until the difference to their row's reference is taken, so that a far reference costs no precision. Probabilities
+// sums are): a vector is multiplied by the power of two that brings its largest element to 1 .. 2. Scores have K's power of two
+// only until the difference to their row's reference is taken, so that a far reference costs no precision. Probabilities
 // P = e^{z - ref} * 2^(V's exponent) * F are rounded to f16 (2^-12 relative): F, a power of two per row, is moved so that
 // they lie below 2^15; the reference is the maximum found when it was last moved. bf16: queries as they are, probabilities
 // rounded to bf16 (2^-9 relative), whose range needs no factor. Sums, references and O are fp32.
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, Shape<HD, NQ, T>::kBlocksPerSm) few_
     auto bytes_of = [&](int id) {
       if (id < 0 || WIDE) return id < 0 ? -1 : kBias | kBias << 8;
       const uint8_t* b = a.scale + static_cast<size_t>(id) * 2 * a.Hkv + hk;
-      return clip_byte(b[0]) | clip_byte(b[a.Hkv]) << 8;
+      return score_byte(b[0]) | clip_byte(b[a.Hkv]) << 8;
     };
     int id0 = id_at(0), id1 = n_list > 32 * kWarps ? id_at(1) : -1, batch = 0;
     auto issue = [&](int i) {                // page i of the warp's into the next stage
@@ -221,11 +221,9 @@ __global__ void __launch_bounds__(kThreads, Shape<HD, NQ, T>::kBlocksPerSm) few_
       uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
-      // (below 2^-100 as if that were the largest: kNone times the scale has to be far beyond every exponent)
-      const int e = min(max(static_cast<int>(__reduce_max_sync(0xffffffffu, top) >> 23), 27), 253);
-      const float down = exp2_byte(254 - e);
-      if (lane < HD / 4) *to = make_uint2(pack_f16(y[0] * down, y[1] * down), pack_f16(y[2] * down, y[3] * down));
-      if (lane == 0) scale_s[x] = __int_as_float(e << 23) * (1.4426950408889634f / sqrtf(static_cast<float>(HD)));
+      const QueryScale f = query_scale(__reduce_max_sync(0xffffffffu, top), HD);
+      if (lane < HD / 4) *to = make_uint2(pack_f16(y[0] * f.down, y[1] * f.down), pack_f16(y[2] * f.down, y[3] * f.down));
+      if (lane == 0) scale_s[x] = f.scale;
     }
 #pragma unroll 1
     for (int i = threadIdx.x; i < kQ * (HD / 32); i += kThreads)
@@ -420,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, Shape<HD, NQ, T>::kBlocksPerSm) few_
               float r = 1.f;
               if (top > ref[n][i]) {
                 r = ex2((ref[n][i] - top) * c0[n][i]);
-                ref[n][i] = top;
+                ref[n][i] = reference(top);
                 sum[n][i] *= r;
               }
               if (WIDE) {

@@ -6,10 +6,12 @@
 #include "quantized.cuh"
 #include "tc.cuh"
 
+#include <float.h>
+
 namespace sd2 {
 namespace q8 {
 
-constexpr float kNone = -3e38f;            // a reference before its row has seen anything
+constexpr float kNone = -FLT_MAX;          // a reference before its row has seen anything
 constexpr float kMaxP = 32768.f, kMaxE = 1048576.f;
 
 struct QAttnArgs {
@@ -39,6 +41,23 @@ __device__ __forceinline__ float ex2(float x) {
 }
 
 __device__ __forceinline__ int exponent(float x) { return static_cast<int>(__float_as_uint(x) >> 23); }   // x >= 0
+
+// Scores of the 8-bit cache. A query vector is multiplied by the power of two that brings its largest element to 1 .. 2, so that
+// it is f16; its products with e4m3 are then below 2 * 448 * 128 < 2^17. They are kept as s * 2^(K's exponent - kDown), which fp32
+// holds under the largest byte (246), with a power of two that is normal under the smallest (10); what takes them to log2 has the
+// query's power and 2^kDown. So scores are right wherever they lie, whatever the two exponents are.
+constexpr int kDown = 9;
+__device__ __forceinline__ int score_byte(int b) { return clip_byte(b) - kDown; }
+// Of a vector whose largest magnitude has the fp32 bits `top`: what it is multiplied by, and scores to log2 (heads of hd). The
+// largest vectors, for which the latter would leave fp32, are brought to up to 2^10 instead of 2.
+struct QueryScale { float down, scale; };
+__device__ __forceinline__ QueryScale query_scale(uint32_t top, int hd) {
+  const int e = min(max(static_cast<int>(top >> 23), 1), 253 - kDown);
+  return {exp2_byte(2 * kBias - e), exp2_byte(e + kDown) * (1.4426950408889634f / sqrtf(static_cast<float>(hd)))};
+}
+// The reference of a row whose largest score so far is `top` (infinities, of a query's or beyond fp32 for the largest vectors, give NaN,
+// as in any softmax).
+__device__ __forceinline__ float reference(float top) { return top < INFINITY ? top : NAN; }
 
 __device__ __forceinline__ float inverse(float x) { return exp2_byte(2 * kBias - exponent(x)); }   // of a power of two
 

@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_attention_kernel(const __gr
       auto bytes_of = [&](int id) {
         if (id < 0) return kBias | kBias << 8;
         const uint8_t* b = a.scale + static_cast<size_t>(id) * 2 * a.Hkv + it.hk;
-        return clip_byte(b[0]) | clip_byte(b[a.Hkv]) << 8;
+        return score_byte(b[0]) | clip_byte(b[a.Hkv]) << 8;
       };
       int id0 = id_at(0), id1 = id_at(1), by0 = bytes_of(id0), by1 = bytes_of(id1);
       for (int j = 0; j < n_tiles && ok; ++j, ++t) {
@@ -364,10 +364,9 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_attention_kernel(const __gr
             larger(y.z);
             larger(y.w);
           }
-          // (below 2^-100 as if that were the largest: kNone times the scale has to be far beyond every exponent)
-          const int e = min(max(static_cast<int>(top >> 23), 27), 253);
-          const float down = exp2_byte(254 - e);
-          scale = __int_as_float(e << 23) * (1.4426950408889634f / sqrtf(static_cast<float>(HD)));
+          const QueryScale f = query_scale(top, HD);
+          const float down = f.down;
+          scale = f.scale;
           if (half < HD / 64) {
             uint32_t h[32];
 #pragma unroll
@@ -449,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_attention_kernel(const __gr
               float move = 0.f;            // log2 of what O is multiplied by
               if (top > ref) {
                 move = (ref - top) * scale;
-                ref = top;
+                ref = reference(top);
                 sum *= ex2(move);
               }
               float p = -INFINITY;         // log2 of the largest product with V's scale
@@ -496,7 +495,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_attention_kernel(const __gr
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                   const float v = exp2_byte(bytes[2 * c + h] >> 8), k = exp2_byte(bytes[2 * c + h] & 255);
-                  const uint64_t k2 = exact ? pair(k, k) : pair(k * scale, k * scale), v2 = exact ? pair(v, v) : pair(v * f, v * f);
+                  const float k_log = fmaxf(k * scale, FLT_MIN);   // (0 would make NaN of masked scores)
+                  const uint64_t k2 = exact ? pair(k, k) : pair(k_log, k_log), v2 = exact ? pair(v, v) : pair(v * f, v * f);
 #pragma unroll
                   for (int i = 0; i < 8; ++i) {
                     uint64_t z = fma2(pair(__uint_as_float(x[c][16 * h + 2 * i]), __uint_as_float(x[c][16 * h + 2 * i + 1])), k2, ref2);
