@@ -517,12 +517,12 @@ __global__ void __launch_bounds__(kThreads, Shape<HD, NQ, T>::kBlocksPerSm) few_
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int x = n * 8 + 2 * c + i;
-        const float weight = coef[warp][x] * inverse(F[n][i]);
+        const float weight = coef[warp][x], back = inverse(F[n][i]);   // (their product may be far below any number)
         const uint32_t to_row = ring + x * (HD * 4);
 #pragma unroll
         for (int k = 0; k < kSteps / 2; ++k)   // the lane's columns 4k .. 4k + 3; chunks of 16 bytes permuted by the row
-          sts128(to_row + (((g * (kSteps / 2) + k) ^ c) * 16), o[n][2 * k][i] * weight, o[n][2 * k][i + 2] * weight,
-                 o[n][2 * k + 1][i] * weight, o[n][2 * k + 1][i + 2] * weight);
+          sts128(to_row + (((g * (kSteps / 2) + k) ^ c) * 16), o[n][2 * k][i] * weight * back, o[n][2 * k][i + 2] * weight * back,
+                 o[n][2 * k + 1][i] * weight * back, o[n][2 * k + 1][i + 2] * weight * back);
       }
     __syncthreads();
 #pragma unroll 1

@@ -264,7 +264,8 @@ struct Walk {
 };
 
 // Joins the parts of each item that was cut: o = sum_z w_z o_z / sum_z w_z, w_z = sum_z * 2^{(ref_z - max) * scale}, in the
-// order of the blocks, four parts in flight. A thread takes four columns of a vector.
+// order of the blocks, four parts in flight, as a running mean (the sum itself could leave fp32). A thread takes four columns of a
+// vector.
 constexpr int kJoinThreads = 256;
 template <int HD, int kQ>
 __global__ void __launch_bounds__(kJoinThreads) quantized_join_kernel(const __grid_constant__ QAttnArgs a) {
@@ -297,22 +298,27 @@ __global__ void __launch_bounds__(kJoinThreads) quantized_join_kernel(const __gr
       next = fmaxf(next, st[k].x);
       scale = fmaxf(scale, st[k].z);       // (0 from a part that saw nothing)
     }
-    const float f = total == 0.f ? 0.f : ex2((top - next) * scale);
+    const float before = total == 0.f ? 0.f : total * ex2((top - next) * scale);
     top = next;
-    total *= f;
-    r.x *= f; r.y *= f; r.z *= f; r.w *= f;
+    total = before;
+    float w[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      if (st[k].y == 0.f) continue;        // (it saw nothing)
-      const float w = st[k].y * ex2((st[k].x - top) * scale);   // (a NaN times a weight of 0 is passed on)
-      total += w;
-      r.x += w * o[k].x; r.y += w * o[k].y; r.z += w * o[k].z; r.w += w * o[k].w;
+      w[k] = st[k].y == 0.f ? 0.f : st[k].y * ex2((st[k].x - top) * scale);
+      total += w[k];
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    r.x *= before * inv; r.y *= before * inv; r.z *= before * inv; r.w *= before * inv;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (st[k].y == 0.f) continue;        // (it saw nothing; any other's NaN is passed on, with a weight of 0, too)
+      const float share = w[k] * inv;
+      r.x += share * o[k].x; r.y += share * o[k].y; r.z += share * o[k].z; r.w += share * o[k].w;
     }
   }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
   const int t = (v0 + x) / a.G, h = hk * a.G + (v0 + x) - t * a.G;
   const size_t to = static_cast<size_t>(row0 + t) * a.H + h;
-  const __nv_bfloat162 lo = __floats2bfloat162_rn(r.x * inv, r.y * inv), hi = __floats2bfloat162_rn(r.z * inv, r.w * inv);
+  const __nv_bfloat162 lo = __floats2bfloat162_rn(r.x, r.y), hi = __floats2bfloat162_rn(r.z, r.w);
   *reinterpret_cast<uint2*>(a.out + to * HD + col * 4) =
       make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
   if (a.lse && col == 0) a.lse[to] = total == 0.f ? -INFINITY : (top * scale + log2f(total)) * 0.6931471805599453f;

@@ -579,7 +579,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_attention_kernel(const __gr
       // The results leave through a panel of 32 rows x 64 bytes (16-byte chunks permuted by the row), so that a store covers
       // 64 bytes of a row.
       const bool none = sum == 0.f || n_tiles == 0;
-      const float inv = none ? 0.f : __fdividef(1.f, sum) * exp2_byte(kBias - F);
+      const float inv = none ? 0.f : __fdividef(1.f, sum), back = exp2_byte(kBias - F);   // (their product may be far below any number)
       const long long item = static_cast<long long>(it.row0 + it.t0 + x_row) * a.H + head;
       const long long out_row = it.part ? static_cast<long long>(it.slot) * kTile + r : item;
       if (half >= HD / 64) continue;       // (64 columns by each thread, those of heads of 64 by the first)
@@ -613,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_attention_kernel(const __gr
         ld_wait(o);
         const uint32_t odd = HD == 128 ? nans[HD / 64 * half + c] : nans[c];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = none ? 0u : odd >> i & 1 ? 0x7FC00000u : __float_as_uint(__uint_as_float(o[i]) * inv);
+        for (int i = 0; i < 32; ++i) o[i] = none ? 0u : odd >> i & 1 ? 0x7FC00000u : __float_as_uint(__uint_as_float(o[i]) * inv * back);
         if (it.part) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {

@@ -152,3 +152,27 @@ def test_the_largest_queries_on_the_largest_keys(way, hd):
     nan = torch.isnan(lse)[..., None].expand(*lse.shape, hd).reshape(out.shape)
     assert torch.equal(torch.isnan(out), nan)
     assert nan.any() and ((lse == float("inf")) | torch.isnan(lse)).all()
+
+
+@pytest.mark.parametrize("power", [-117, 119])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("way,claim", [("few", 6000), ("few", 64), ("tiles", 1 << 20)])
+def test_values_at_the_ends_of_the_exponents(way, claim, hd, power):
+    """V under the smallest or the largest exponent, with scores that rise after the first pages by less than moves a row's reference, so
+    that its sum is far above 1; items cut into parts, and (a cache that is said to be short) a whole one."""
+    c = paged.case([1] if way == "few" else [12], [6000], 8, 2, hd, seed=1, eight=True, spread=0.0)
+    ids = c["table"][0, : 375].long()
+    c["scale"][c["layer"], ids, 1] = paged.BIAS + power
+    c["pool"].view(torch.uint8)[c["layer"], ids, 1] &= 0x7F                # (no sums that cancel)
+    k = torch.full((6000, 2, hd), 8.6 / (4 * hd ** 0.5))
+    k[:256] = 0.0                           # (the first two pages of each of a block's eight warps)
+    pool, scale = paged.quantized(k.view(375, 16, 2, hd).transpose(1, 2))
+    c["pool"].view(torch.uint8)[c["layer"], ids, 0] = pool.view(torch.uint8)
+    c["scale"][c["layer"], ids, 0] = scale
+    c["q"] = torch.full_like(c["q"], 4.0)
+    o, l, mag = paged.definition(c)
+    out, lse, err = run_case(c, max_kv=claim)
+    assert err == 0
+    assert (lse.double() - l).abs().max() <= 4e-4
+    # (a result near 2^-117 is a normal bf16 number or off by at most half the smallest subnormal, 2^-134)
+    assert ((out.double() - o).abs() <= 2 ** -8 * o.abs() + (2 ** -11 + 2e-4) * mag + 2.0 ** -134).all()
