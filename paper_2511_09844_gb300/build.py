@@ -3,7 +3,8 @@
 Each translation unit under csrc/ is compiled in parallel to an object, then linked into
 paper_2511_09844_gb300/_lib/libsd2.so. A rebuild happens only when a source or header is newer
 than the library. No torch extension machinery is used: the library has a plain C ABI. Beside it
-the compiled part of the Python binding (csrc/binding.cpp) is built with g++ against torch's headers.
+the compiled part of the Python binding (csrc/binding.cpp) is built with g++ against torch's headers; where that cannot
+be done (no torch, no headers), the binding makes its calls through ctypes.
 """
 from __future__ import annotations
 
@@ -13,13 +14,13 @@ import shutil
 import subprocess
 import sys
 import sysconfig
+from importlib import metadata
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OUT_DIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(OUT_DIR, "libsd2.so")
-BINDING = os.path.join(OUT_DIR, "sd2_binding.so")
 SOURCES = ["engine.cu", "gemm_simt.cu", "gemm_tc.cu", "attention.cu", "norm.cu", "sampling.cu", "state.cu", "noalloc.cu", "chain.cu",
            "pages.cu", "prompt_attention.cu", "quantized_pages.cu", "quantized_attention.cu", "few_rows.cu",
            "quantized_tiles.cu"]
@@ -42,32 +43,69 @@ def _inputs():
     return files
 
 
+def binding_path():
+    """The binding's compiled part for this Python and torch (one of another torch may load and not fit), None without torch."""
+    try:
+        version = metadata.version("torch")
+    except metadata.PackageNotFoundError:
+        return None
+    return os.path.join(OUT_DIR, f"sd2_binding-{version}-{sys.implementation.cache_tag}.so")
+
+
+def _failed(binding: str) -> str:
+    """Stands in the place of a binding that could not be compiled, so that this is not tried at every build."""
+    return binding + ".failed"
+
+
 def is_stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(BINDING):
+    made, binding = [LIB], binding_path()
+    if binding is not None:
+        made.append(binding if os.path.exists(binding) else _failed(binding))
+    if not all(map(os.path.exists, made)):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
+    t = min(map(os.path.getmtime, made))
     return any(os.path.getmtime(f) > t for f in _inputs())
 
 
 def _build_binding() -> None:
+    """Compile binding.cpp if that can be done; the reason is reported if not."""
+    binding = binding_path()
+    if binding is None:
+        return
+    try:
+        _compile_binding(binding)
+        why = None
+    except (ImportError, OSError, RuntimeError) as e:
+        why = str(e)
+        sys.stderr.write(f"binding.cpp is left out, calls go through ctypes: {why}\n")
+    if why is None and os.path.exists(_failed(binding)):
+        os.remove(_failed(binding))
+    if why is not None:
+        if os.path.exists(binding):          # (of older sources)
+            os.remove(binding)
+        with open(_failed(binding), "w") as f:
+            f.write(why)
+
+
+def _compile_binding(binding: str) -> None:
     import torch
     home = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
     dirs = [os.path.join(ROOT, "include"), os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
             os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
-    lib, tmp = os.path.join(home, "lib"), BINDING + ".tmp"
+    lib, tmp = os.path.join(home, "lib"), binding + ".tmp"
     cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            *(f"-I{d}" for d in dirs), os.path.join(CSRC, "binding.cpp"), "-o", tmp, f"-L{lib}", "-ltorch_python", "-ltorch",
            "-ltorch_cpu", "-lc10", "-lc10_cuda", f"-Wl,-rpath,{lib}"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode:
-        sys.stderr.write(r.stdout + r.stderr)
-        raise RuntimeError("g++ failed on binding.cpp")
-    os.replace(tmp, BINDING)
+        raise RuntimeError("g++ failed\n" + r.stdout + r.stderr)
+    os.replace(tmp, binding)
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
-    """Compile and link libsd2.so, and the binding; returns the library's path. Raises on any compiler error."""
+    """Compile and link libsd2.so, and the binding where it can be; returns the library's path. Raises on any error of the
+    library's."""
     if not force and not is_stale():
         return LIB
     os.makedirs(OUT_DIR, exist_ok=True)

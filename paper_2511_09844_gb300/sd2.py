@@ -10,11 +10,13 @@ import ctypes
 import functools
 import importlib.util
 import os
+import warnings
 from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
 from typing import List, NamedTuple, Optional, Sequence
 
 import torch
 
+from . import build
 from .workloads import LAYER_SLOTS, PairWorkload
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_lib", "libsd2.so")
@@ -164,16 +166,20 @@ _native = None
 
 
 def _connect():
-    """The compiled part of the binding (csrc/binding.cpp), False where it has not been built: the calls that it answers are
-    then made here, which takes 20 us of host time instead of 6."""
+    """The compiled part of the binding (csrc/binding.cpp), False where it has not been built or does not load: the calls that
+    it answers are then made here, which takes 20 us of host time instead of 6."""
     global _native
-    lib, path = load_library(), os.path.join(os.path.dirname(LIB_PATH), "sd2_binding.so")
-    if not os.path.exists(path):
-        _native = False
+    lib, path = load_library(), build.binding_path()
+    _native = False
+    if path is None or not os.path.exists(path):
         return _native
-    spec = importlib.util.spec_from_file_location("sd2_binding", path)
-    module = importlib.util.module_from_spec(spec)
-    spec.loader.exec_module(module)
+    try:
+        spec = importlib.util.spec_from_file_location("sd2_binding", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError as e:
+        warnings.warn(f"sd2_binding does not load, calls go through ctypes: {e}", RuntimeWarning)
+        return _native
     module.connect(*(ctypes.cast(f, c_void_p).value for f in (
         lib.sd2_attention_window, lib.sd2_attention_window_workspace_bytes, lib.sd2_attention_quantized,
         lib.sd2_attention_quantized_workspace_bytes, lib.sd2_pages_append_quantized)))
