@@ -486,8 +486,10 @@ sd2_status sd2_pages_append_quantized(const void* d_k, int64_t ldk, const void* 
  * if window is not 0. A NaN of the cache reaches the rows that see its position, no others. Of few rows, scores may lie
  * anywhere, also beyond fp32 (lse is infinite there); of prompts, q . k has to lie in fp32, with elements of q above 2^-110 (a row's
  * largest beyond it gives NaN). d_workspace:
- * sd2_attention_quantized_workspace_bytes(..) bytes, else as there; for prompts this includes a bf16 copy of the layer's
- * pages, as long as that is at most 4 GB. */
+ * sd2_attention_quantized_workspace_bytes(..) bytes, else as there; for prompts this includes a bf16 copy of pages: of the layer's
+ * (up to 512 MB, or where twice as many can be seen as it has), or of those that sequences of max_kv positions can see through the
+ * window. Up to 4 GB; of a pool that would take more as bf16, up to 128 MB. Calls that see more take a way without copies, which for
+ * prompts takes up to twice as long. */
 size_t sd2_attention_quantized_workspace_bytes(int32_t M, int32_t n_seq, int32_t H, int32_t Hkv, int32_t hd,
                                                int32_t max_kv, int32_t n_blocks, int32_t window, int32_t sinks);
 sd2_status sd2_attention_quantized(const void* d_q, int64_t ldq, int32_t M, int32_t H, int32_t Hkv, int32_t hd,

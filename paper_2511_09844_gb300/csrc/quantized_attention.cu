@@ -22,21 +22,48 @@ using namespace q8;
 
 constexpr int kThreads = 256;
 
-// The pages that some row sees, of the layer's pool, as bf16 under the same page ids: exact, since a value has four
-// significant bits and any exponent is a bf16 one. A block takes a page at a time; pages are numbered in the order of the
-// sequences, 32 of which a warp looks through at once. A shared page is written more than once, with the same values.
-template <int HD>
-__global__ void __launch_bounds__(kThreads) widen_pages_kernel(const QAttnArgs a, const uint8_t* pool, bf16* to) {
+// Where widened pages go if not under their ids: page i of those that sequence s sees is page s * room + i, and `table`
+// [n_seq][columns] names them. A sequence that sees more pages than `room`, or one beyond the columns (its length is more than the
+// call was told), cannot go there: none do then. Of the row offsets, `cu` are all zeros in that case, `rest` in the other.
+struct Dense {
+  int room, columns;                       // room 0: widened under the same ids
+  int *table, *cu, *rest;                  // (null: no sequence can be too long)
+};
+
+// The pages that some row sees, of the layer's pool, as bf16: exact, since a value has four significant bits and any exponent
+// is a bf16 one. A block takes a page at a time; pages are numbered in the order of the sequences, 32 of which a warp looks
+// through at once. Under the same ids a shared page is written more than once, with the same values; DENSE, a sequence shares
+// what it has in common with the first one of its 32 that has the same first page.
+template <int HD, bool DENSE>
+__global__ void __launch_bounds__(kThreads, 8) widen_pages_kernel(const QAttnArgs a, const uint8_t* pool, bf16* to, const Dense d) {
   const int lane = threadIdx.x & 31;
-  unsigned next = blockIdx.x, before = 0;
+  const unsigned spare = DENSE && d.rest ? 1 : 0, blocks = gridDim.x - spare;   // one block is for the offsets
+  unsigned next = blockIdx.x - spare, before = 0;
   pdl_wait();
+  if (DENSE && blockIdx.x < spare) {
+    int over = 0;
+    for (int s = threadIdx.x; s < a.n_seq; s += kThreads) {
+      const Seq f = load_seq<1>(a, s);
+      over |= f.rows > 0 && (f.pages > d.room || (f.kv + kPage - 1) / kPage > d.columns);
+    }
+    over = __syncthreads_or(over);
+    for (int s = threadIdx.x; s <= a.n_seq; s += kThreads) {
+      d.cu[s] = over ? 0 : a.cu[s];
+      d.rest[s] = over ? a.cu[s] : 0;
+    }
+    return;
+  }
   for (int s0 = 0; s0 < a.n_seq; s0 += 32) {
     Seq f{};
     unsigned n = 0;
+    int head = 0;
     if (s0 + lane < a.n_seq) {
+      if (DENSE) head = a.table[static_cast<size_t>(s0 + lane) * a.bt_stride];
       f = load_seq<1>(a, s0 + lane);
       if (f.rows > 0 && f.kv > 0) n = f.pages;
     }
+    int twin = lane;
+    if (DENSE) twin = __ffs(__match_any_sync(0xffffffffu, n ? head : -1 - lane)) - 1;
     unsigned upto = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -44,17 +71,30 @@ __global__ void __launch_bounds__(kThreads) widen_pages_kernel(const QAttnArgs a
       if (lane >= o) upto += t;
     }
     const unsigned all = before + __shfl_sync(0xffffffffu, upto, 31);
-    for (; next < all; next += gridDim.x) {
+    for (; next < all; next += blocks) {
       const int src = __ffs(__ballot_sync(0xffffffffu, before + upto > next)) - 1;
       const int i = static_cast<int>(next - before - __shfl_sync(0xffffffffu, upto - n, src));
       const int page = i + (i >= __shfl_sync(0xffffffffu, f.sp, src) ? __shfl_sync(0xffffffffu, f.gap, src) : 0);
       const int id = a.table[static_cast<size_t>(s0 + src) * a.bt_stride + page];
-      if (id < 0 || id >= a.n_blocks) continue;       // (attention reports it)
+      const bool there = id >= 0 && id < a.n_blocks;  // (attention reports those that are not)
+      int slot = id;
+      if (DENSE) {
+        if (i >= d.room || page >= d.columns) continue;   // (a sequence that is too long)
+        // (`mine`: of each lane's sequence, the number of its page `page`, if it sees that)
+        int owner = __shfl_sync(0xffffffffu, twin, src), mine = page < f.sp ? page : page - f.gap;
+        if ((page >= f.sp && mine < f.sp) || mine >= min(static_cast<int>(n), d.room)) mine = -1;
+        if (owner != src && (__shfl_sync(0xffffffffu, mine, owner) < 0 || a.table[static_cast<size_t>(s0 + owner) * a.bt_stride + page] != id))
+          owner = src;
+        slot = (s0 + owner) * d.room + __shfl_sync(0xffffffffu, mine, owner);
+        if (threadIdx.x == 0) d.table[static_cast<size_t>(s0 + src) * d.columns + page] = there ? slot : -1;
+        if (owner != src) continue;
+      }
+      if (!there) continue;
       const int vecs = 2 * a.Hkv * HD;                // of 16 values
       const uint4* x = reinterpret_cast<const uint4*>(pool + static_cast<size_t>(id) * vecs * 16);
-      uint4* y = reinterpret_cast<uint4*>(to + static_cast<size_t>(id) * vecs * 16);
+      uint4* y = reinterpret_cast<uint4*>(to + static_cast<size_t>(slot) * vecs * 16);
       const uint8_t* bytes = a.scale + static_cast<size_t>(id) * 2 * a.Hkv;
-#pragma unroll 4
+#pragma unroll (DENSE ? 2 : 4)               // (32 registers, 8 blocks on an SM: with 4 and spills 2 us more)
       for (int v = threadIdx.x; v < vecs; v += kThreads) {
         const uint4 w = ld_stream(x + v);
         const float scale = exp2_byte(clip_byte(bytes[v / HD]));
@@ -81,18 +121,26 @@ __global__ void __launch_bounds__(kThreads) widen_pages_kernel(const QAttnArgs a
 struct Plan {
   int kq, blocks, items;                   // query vectors of an item (bf16: 0 for prompt attention); blocks of the grid; items, at most
   bool split;
-  size_t widened;                          // prompts: bytes of the layer's pool as bf16, else 0
+  size_t widened;                          // prompts: bytes of the widened pages and their tables, else 0
+  int room, columns;                       // Dense
 };
-// Prompts widen the pages they see to bf16 and go through prompt attention, while the layer's pool as bf16 is at most
-// kMostWidened bytes: from kPrompt query vectors of a KV head per sequence on, on average, or from more than kLongPrompt on where
-// that many pages times KV heads (kLong) are likely to be seen, since widening then costs as much as two or three passes of tiles
-// of 128 vectors. In us, by tiles and by prompts: 4 sequences of 60000, 8/8 heads of 128, 128 vectors 168 and 427, 384 460 and
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+// Prompts widen the pages they see to bf16 and go through prompt attention. Where: under the pool's ids; or, of a pool beyond
+// kSmallPool bytes as bf16, and where it takes less than half of them, under numbers of their own, which go by what the call can see:
+// 16 sequences of 1000 positions, 8 heads of 128, in a pool of 60000 pages 63 MB instead of 3750, four chunks on 3K-16K 262. That
+// takes 2 us more for the numbers and the table, and 4 for a kernel that is there for lengths beyond what the call was told, if the
+// table has room for such (16 x 64 rows on 1000 39.0 -> 40.6 or 44.9 us, 2048 rows 47.4 -> 49.0 or 51.5, four chunks on 3K-16K
+// 312-321 -> 315 or 327, 8 x 400 rows through 1024 68 -> 77), and saves the widening of shared pages (16 x 300 rows behind 8192 shared
+// positions 519 -> 452). At most
+// kMostWidened bytes, or kMostOfLarge of a pool that would itself take more: beyond, by tiles (these chunks 587, 16 x 64 rows 63).
+// When: from kPrompt query vectors of a KV head per sequence on, on average, or from more than long_prompt on where that many pages
+// times KV heads (kLong) are likely to be seen, since widening then costs as much as two or three passes of tiles of 128 vectors. In us, by tiles and by prompts: 4 sequences of 60000, 8/8 heads of 128, 128 vectors 168 and 427, 384 460 and
 // 807, 1024 1181 and 817; 16 of 8000, 256 vectors 193 and 230, 384 282 and 295, 512 357 and 313; 16 of 1000, 256 61 and 38; 2/2
 // heads of 64, 4 of 60000, 256 vectors 82 and 100, 512 145 and 124, 4 of 8000, 256 27.5 and 27.4.
 constexpr int kPrompt = 128;
 constexpr int kLong = 8192;
 constexpr int long_prompt(int hd) { return hd == 64 ? 256 : 384; }
-constexpr size_t kMostWidened = 4ull << 30;
+constexpr size_t kMostWidened = 4ull << 30, kMostOfLarge = 128ull << 20, kSmallPool = 512ull << 20;
 constexpr int kShare = 32;                 // least cost of a share
 constexpr int kJoinCost = 28;              // the join, in pages of a block
 long long vectors_of(int M, int n_seq, int H, int Hkv) {   // of a sequence, on average
@@ -121,6 +169,8 @@ double prompt_us(double vectors, double lists, Seen seen, int hd, bool wide) {
   const double bf16_us = hd == 64 ? 7 + 0.005 * lists : 8 + 0.02 * lists;
   return wide ? bf16_us + walk : bf16_us + (hd == 64 ? 3 : 6) + walk + lists * seen.mean * (hd == 64 ? 0.001 : 0.002);
 }
+// Of Dense: the table, and two arrays of row offsets.
+size_t dense_tables(long long n_seq, long long columns) { return round256(n_seq * columns * 4) + 2 * round256((n_seq + 1) * 4); }
 // wide: the bf16 cache, whose pages take twice as long
 Plan plan_of(int M, int n_seq, int H, int Hkv, int hd, int max_kv, int n_blocks, int window, int sinks, bool wide = false) {
   Plan p{};
@@ -131,7 +181,20 @@ Plan plan_of(int M, int n_seq, int H, int Hkv, int hd, int max_kv, int n_blocks,
   const long long rows = (M + n_seq - 1) / n_seq;
   const long long seen = window ? std::min<long long>(max_kv, static_cast<long long>(window) + sinks + rows) : max_kv;
   const long long pages = (seen + kPage - 1) / kPage;   // of the longest sequence
-  p.widened = static_cast<size_t>(n_blocks) * 2 * Hkv * kPage * hd * 2;
+  const size_t page_bytes = static_cast<size_t>(2) * Hkv * kPage * hd * 2;
+  p.widened = n_blocks * page_bytes;
+  // what a sequence of at most M rows sees: the first positions' pages and those from its first row's window on
+  const long long columns = (static_cast<long long>(max_kv) + kPage - 1) / kPage;
+  const long long room = window ? std::min(columns, (static_cast<long long>(sinks) + kPage - 1) / kPage +
+                                                        (static_cast<long long>(window) + M + kPage - 2) / kPage + 2) : columns;
+  if (p.widened > kSmallPool && n_seq * room <= n_blocks / 2) {
+    const size_t dense = round256(n_seq * room * page_bytes) + dense_tables(n_seq, columns);
+    if (2 * dense <= p.widened && dense <= (p.widened <= kMostWidened ? kMostWidened : kMostOfLarge)) {
+      p.widened = dense;
+      p.room = static_cast<int>(room);
+      p.columns = static_cast<int>(columns);
+    }
+  }
   const bool many = static_cast<long long>(n_seq) * Hkv * (pages * 2 / 3) >= kLong ? vectors > long_prompt(hd) : vectors >= kPrompt;
   if (wide || !many || p.widened > kMostWidened) p.widened = 0;
   // Items of 8 or 16 vectors, several of a sequence, where they are likely to take less time even if all caches are as long as the
@@ -167,7 +230,6 @@ Plan plan_of(int M, int n_seq, int H, int Hkv, int hd, int max_kv, int n_blocks,
   p.blocks = static_cast<int>(p.split ? slots : p.items);
   return p;
 }
-size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 size_t items_bytes(const Plan& p) { return round256((1 + 2 * static_cast<size_t>(p.items)) * 16); }
 size_t parts_bytes(const Plan& p, int hd) {
   return p.split ? items_bytes(p) + round256(2 * static_cast<size_t>(p.blocks) * p.kq * (hd + 4) * 4) : 0;
@@ -280,16 +342,38 @@ sd2_status sd2_attention_quantized(const void* d_q, int64_t ldq, int32_t M, int3
   if (p.widened) {
     const int grid = 8 * sm_count_cached();
     bf16* wide = reinterpret_cast<bf16*>(work);
-    e = launch_pdl(hd == 128 ? widen_pages_kernel<128> : widen_pages_kernel<64>, dim3(grid), dim3(kThreads), 0, st, a, pool, wide);
+    Dense d{};
+    if (p.room) {
+      d.room = p.room;
+      d.columns = std::min(p.columns, bt_stride);
+      const size_t offsets = round256((static_cast<size_t>(n_seq) + 1) * 4);
+      unsigned char* const tables = work + p.widened - dense_tables(n_seq, p.columns);
+      d.table = reinterpret_cast<int*>(tables + 2 * offsets);
+      if (bt_stride > p.columns) {
+        d.cu = reinterpret_cast<int*>(tables);
+        d.rest = reinterpret_cast<int*>(tables + offsets);
+      }
+    }
+    auto widen = [&](auto kernel) { return launch_pdl(kernel, dim3(grid), dim3(kThreads), 0, st, a, pool, wide, d); };
+    e = hd == 128 ? (p.room ? widen(widen_pages_kernel<128, true>) : widen(widen_pages_kernel<128, false>))
+                  : (p.room ? widen(widen_pages_kernel<64, true>) : widen(widen_pages_kernel<64, false>));
     if (e == cudaSuccess) {
       PromptAttnArgs pa{};
       pa.q = d_q; pa.ldq = ldq; pa.M = M; pa.H = H;
-      pa.kv.pool = wide; pa.kv.table = d_table; pa.kv.bt_stride = bt_stride; pa.kv.n_blocks = n_blocks;
-      pa.kv.Hkv = Hkv; pa.kv.hd = hd;
-      pa.cu = d_cu_rows; pa.kv_len = d_kv_len; pa.n_seq = n_seq; pa.max_kv = max_kv;
+      pa.kv.pool = wide; pa.kv.Hkv = Hkv; pa.kv.hd = hd;
+      pa.kv.table = p.room ? d.table : d_table;
+      pa.kv.bt_stride = p.room ? d.columns : bt_stride;
+      pa.kv.n_blocks = p.room ? n_seq * p.room : n_blocks;
+      pa.cu = d.rest ? d.cu : d_cu_rows; pa.kv_len = d_kv_len; pa.n_seq = n_seq; pa.max_kv = max_kv;
       pa.window = std::min(window, 1 << 30); pa.sinks = std::min(sinks, 1 << 30);
       pa.out = d_out; pa.lse = d_lse; pa.work = work + round256(p.widened); pa.err = a.err;
       e = prompt_attention(pa, st);
+    }
+    if (e == cudaSuccess && d.rest) {      // whole items, a few per block; nothing, where all went through prompt attention
+      a.cu = d.rest;
+      a.min_share = 0;
+      a.rest = true;
+      e = quantized_attention_tiles(a, pool, hd, sm_count_cached(), st);
     }
     return e == cudaSuccess ? SD2_OK : fail(SD2_ECUDA, std::string("attention launch: ") + cudaGetErrorString(e));
   }

@@ -25,13 +25,14 @@ struct QAttnArgs {
   int n_seq, window, sinks;                // window 2^30: none
   bf16* out;
   float* lse;
-  int max_items, min_share;                // items the workspace has room for; least cost of a block's share, 0: it takes one
-                                           // whole item
+  int max_items, min_share;                // items the workspace has room for; least cost of a block's share, 0: it takes
+                                           // whole items
   float* part_o;                           // [2 blocks][kQ][hd]: normalised results of parts of an item
   float4* part_st;                         // [2 blocks][kQ]: reference, sum, scale to log2
   int4* items;                             // [1 + 2 items]: their number and a block's share; first block, first packed row,
                                            // first vector, vectors; KV head, place of the last page in all work
   unsigned* err;
+  bool rest;                               // rows that another kernel may have left: usually none, all offsets are 0 then
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -119,7 +120,8 @@ constexpr int kItemCostFew = 48, kItemCostFewWide = 24, kItemCostTiles = 32;
 // Work: an item is a tile of kQ query vectors (token-major: vector v of a sequence is head v % G of its row v / G) of one
 // sequence and KV head. All items, in the order of sequences, KV heads and tiles, cost kItemCost.. and their pages, counted in
 // units of kUnit pages; each block takes an equal share of that (one per resident slot of the GPU, so that ragged lengths
-// level out), which cuts some items into parts that a second kernel joins; or, where the caches are short, one whole item.
+// level out), which cuts some items into parts that a second kernel joins; or, where the caches are short, whole items (one, if
+// there are as many blocks).
 struct Item {
   int seq, row0, hk, v0, nv;               // sequence, its first packed row, KV head, first vector of the tile, vectors
   int t0, r0;                              // row and head of the first vector
@@ -176,7 +178,7 @@ struct Walk {
       if (lane == 0) atomicOr(a.err, static_cast<unsigned>(ERR_RANGE));
       all = all_tiles = 0;
     }
-    const unsigned share = whole ? 1u : max(static_cast<unsigned>(a.min_share / kUnit), (all + gridDim.x - 1) / gridDim.x);
+    const unsigned share = max(whole ? 1u : static_cast<unsigned>(a.min_share / kUnit), (all + gridDim.x - 1) / gridDim.x);
     begin = blockIdx.x * share;
     end = min(all, begin + share);
     if (!whole && blockIdx.x == 0) {

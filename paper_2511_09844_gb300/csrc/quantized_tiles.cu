@@ -100,6 +100,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_attention_kernel(const __gr
   // raw tiles, f16 tiles, panels
   const uint32_t raw0 = smem_u32(smem) + kWideS * Lay::kWide, wide0 = smem_u32(smem), panels = raw0 + kRawS * Lay::kRaw;
   volatile int* abort_flag = flags;
+  if (a.rest) {
+    pdl_wait();
+    if (a.cu[a.n_seq] == 0) return;
+  }
   if (a.min_share) pdl_trigger();          // the join may be set up (it waits for this grid to complete)
   if (threadIdx.x == 0) {
     flags[0] = 0;
