@@ -26,13 +26,7 @@ __device__ __forceinline__ int byte_for(uint32_t top) {
   return clip_byte(static_cast<int>(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0));
 }
 
-// Two e4m3 values (low byte first) as f16, exactly.
-__device__ __forceinline__ uint32_t to_f16x2(uint32_t two) {
-  uint32_t r;
-  asm("{\n .reg .b16 h;\n cvt.u16.u32 h, %1;\n cvt.rn.f16x2.e4m3x2 %0, h;\n}" : "=r"(r) : "r"(two));
-  return r;
-}
-// The four e4m3 values of a word as two f16 pairs.
+// The four e4m3 values of a word as two f16 pairs, exactly.
 __device__ __forceinline__ void to_f16x4(uint32_t four, uint32_t& lo, uint32_t& hi) {
   asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}"
       : "=r"(lo), "=r"(hi)
