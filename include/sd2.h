@@ -454,7 +454,8 @@ sd2_status sd2_pages_compact(void* d_pool, int32_t L, int32_t n_blocks, int32_t 
                              void* d_workspace, size_t workspace_bytes, uint32_t* d_err, void* stream);
 
 /* sd2_attention_prompt through a sliding window: a row at position p sees the positions j <= p that are above p - window,
- * or below sinks (the first ones, which stay visible). K/V tiles that no row of theirs sees are not read. window >= 1,
+ * or below sinks (the first ones, which stay visible). K/V tiles that no row of theirs sees are not read. Few query vectors per
+ * sequence on average go through a kernel of their own, so that one's last bits may change with the others of its batch. window >= 1,
  * sinks >= 0 (SD2_EINVAL); all else as there, with workspaces of sd2_attention_window_workspace_bytes(.., window, sinks). */
 size_t sd2_attention_window_workspace_bytes(int32_t M, int32_t n_seq, int32_t H, int32_t Hkv, int32_t hd,
                                             int32_t max_kv, int32_t window, int32_t sinks);
@@ -469,7 +470,10 @@ sd2_status sd2_attention_window(const void* d_q, int64_t ldq, int32_t M, int32_t
  * (1 sign, 4 exponent and 3 mantissa bits; largest 448, no infinity) [L][n_blocks][2 (K, V)][Hkv][16][hd], with an
  * exponent byte for each page, K or V, and head in d_scale [L][n_blocks][2][Hkv]: a value stands for
  * e4m3 * 2^(byte - 127). Bytes outside 10 .. 246 count as the nearest of these. Tables, batches and the error word are
- * those of the bf16 cache.
+ * those of the bf16 cache. sd2_pages_fork and sd2_pages_compact take its values as 16-bit words (hd / 2 in place of hd) and do not
+ * know the bytes: for every page that they copy or move the caller copies its bytes in d_scale, in all layers, after the call (a
+ * forked tail: from the parent's page at that place to the new table's; compact: by d_map). Without them a copied page's values
+ * are off by powers of two, and no call can tell.
  * ------------------------------------------------------------------------------------------- */
 
 /* sd2_pages_append to the 8-bit cache. A block (a page's rows of one head, K or V) that gets new rows with the largest
@@ -485,7 +489,9 @@ sd2_status sd2_pages_append_quantized(const void* d_k, int64_t ldk, const void* 
 /* sd2_attention_prompt over the 8-bit cache, of prompts as of single tokens; through a window as in sd2_attention_window
  * if window is not 0. A NaN of the cache reaches the rows that see its position, no others. Of few rows, scores may lie
  * anywhere, also beyond fp32 (lse is infinite there); of prompts, q . k has to lie in fp32, with elements of q above 2^-110 (a row's
- * largest beyond it gives NaN). d_workspace:
+ * largest beyond it gives NaN). Which way a call takes goes by the query vectors (rows x heads per KV head) of its sequences, on average,
+ * and by max_kv; probabilities are rounded to f16 in the ways of few vectors (by 2^-12), to bf16 in that of prompts (by 2^-9), so
+ * that one sequence's last bits may change with the others of its batch. d_workspace:
  * sd2_attention_quantized_workspace_bytes(..) bytes, else as there; for prompts this includes a bf16 copy of pages: of the layer's
  * (up to 512 MB, or where twice as many can be seen as it has), or of those that sequences of max_kv positions can see through the
  * window. Up to 4 GB; of a pool that would take more as bf16, up to 128 MB. Calls that see more take a way without copies, which for

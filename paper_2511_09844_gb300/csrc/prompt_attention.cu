@@ -43,7 +43,7 @@
 // Windows (a row sees the `window` positions up to its own and the first `sinks` ones): a piece's positions are counted
 // without the whole pages that none of its rows sees, so that its tiles hold the first positions and the window back to back
 // and the loops are as before; masks are set on tiles with an end of some row's window. Measured: 16384 rows, 32/8 heads of
-// 128, through 4096 positions, 600 us, 1.60 PFLOP/s of visible pairs (685 with the tiles of the whole sequence that lie in
+// 128, through 4096 positions, 584-623 us, 1.55-1.65 PFLOP/s of visible pairs (685 with the tiles of the whole sequence that lie in
 // the window); 24 prompts of 1-2100 rows, 32/8 heads of 64, through 257, 57.5 us (63.6). Without a window (a variant of its own)
 // nothing has changed. Few rows go through few_rows.cu.
 #include "sd2.h"

@@ -3,7 +3,7 @@
 // Three ways, by the query vectors that a KV head has per sequence (rows x heads per KV head, on average): up to 24 or 32, whose
 // bound is the cache's bytes, few_rows.cu; up to 127 (256 or 384 on long caches), quantized_tiles.cu; and prompts, bound by their products: the pages they
 // see are widened to bf16 and go through prompt attention. Four chunks of 411-777 rows on 3K-16K positions, 40/8 heads of
-// 128, take 373 us so (385 with 16-byte stores of the widened pages), and took 2442 in the first kernel, which took every row
+// 128, take 371 us so (385 with 16-byte stores of the widened pages), and took 2442 in the first kernel, which took every row
 // as few_rows.cu does.
 #include "sd2.h"
 #include "quantized_attention.cuh"
@@ -147,7 +147,10 @@ long long vectors_of(int M, int n_seq, int H, int Hkv) {   // of a sequence, on 
   return static_cast<long long>((M + n_seq - 1) / n_seq) * (H / Hkv);
 }
 // Estimated times in us, for the choice between many small items and few large ones where both leave SMs idle: a call on a page
-// or two, and what each further page of a block adds.
+// or two, and what each further page of a block adds. Fitted to calls of one sequence with 2 and 8 KV heads from a graph, whole
+// items; of 8 vectors these take 5.1 us and 0.061 a page (heads of 64) or 5.7 and 0.085 (128), over the bf16 cache 4.7 and 0.059 or
+// 4.9 and 0.092. Those of prompts are rough: within a third for up to 64 rows, half of what 16 sequences of 200 rows on 1000
+// positions take. That is on the side of prompts; the choices that this rests on are measured below, in plan_of.
 struct Rate { double base, page; };
 Rate rate_of(int kq, int hd, bool wide) {
   if (wide) return kq == 8 ? (hd == 64 ? Rate{4.3, 0.07} : Rate{4.9, 0.10}) : (hd == 64 ? Rate{5.6, 0.08} : Rate{6.4, 0.12});

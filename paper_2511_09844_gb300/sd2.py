@@ -785,7 +785,8 @@ def pages_append_quantized(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor,
                            err: Optional[torch.Tensor] = None, stream=None) -> None:
     """Write packed K/V rows to their pages of one layer of a cache held in 8 bits (sd2_pages_append_quantized). pool
     float8_e4m3fn [L, n_blocks, 2, Hkv, 16, hd], scale uint8 [L, n_blocks, 2, Hkv]: a value stands for
-    e4m3 * 2^(scale - 127). k, v and the batch as in pages_append."""
+    e4m3 * 2^(scale - 127). k, v and the batch as in pages_append. pages_fork and pages_compact of such a cache take
+    pool.view(torch.bfloat16) and leave scale alone: copy the bytes of the pages that they copy or move."""
     if stream is not None:
         return _within(stream, None, pages_append_quantized, k, v, pool, scale, table, layer, cu_rows, kv_len, err)
     native = _connect() if _native is None else _native

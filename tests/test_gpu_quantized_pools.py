@@ -179,3 +179,25 @@ def test_a_short_prompt_in_a_pool_beyond_4_gb():
     assert need_of(c, 400, n) < 64 << 20
     want, got = run(c), run(c, n)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("rows,kv", [([1, 2, 1], [500, 3000, 40]), ([150, 300], [300, 1200])])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_a_compacted_cache(hd, rows, kv):
+    """Values as 16-bit words through pages_compact, the exponent bytes by its map: the same results."""
+    c = paged.case(rows, kv, 8, 2, hd, seed=6, eight=True)
+    d = on_device(c, 700)
+    pages = torch.tensor([(x + 15) // 16 for x in kv], dtype=torch.int32)
+    ref = torch.zeros(700, dtype=torch.int32)
+    for s, n in enumerate(pages):
+        ref[d["table"][s, :n].cpu().long()] += 1
+    want = run(c)
+    got = sd2.pages_compact(d["pool"].view(torch.bfloat16), d["table"], pages.cuda(), ref.cuda())
+    old = torch.nonzero(got.map >= 0)[:, 0]
+    scale = d["scale"].clone()
+    scale[:, got.map[old].long()] = d["scale"][:, old]
+    n = int(got.n_live)
+    assert n == int(pages.sum()) and int(got.table.max()) < n
+    out, lse = sd2.attention_quantized(d["q"], d["pool"][:, :n].contiguous(), scale[:, :n].contiguous(), got.table, c["layer"], d["cu"], d["kv_len"],
+                                       max_kv=max(kv), return_lse=True)
+    assert torch.equal(out.cpu(), want[0]) and torch.equal(lse.cpu(), want[1])
