@@ -493,7 +493,7 @@ sd2_status sd2_pages_append_quantized(const void* d_k, int64_t ldk, const void* 
  * and by max_kv; probabilities are rounded to f16 in the ways of few vectors (by 2^-12), to bf16 in that of prompts (by 2^-9), so
  * that one sequence's last bits may change with the others of its batch. d_workspace:
  * sd2_attention_quantized_workspace_bytes(..) bytes, else as there; for prompts this includes a bf16 copy of pages: of the layer's
- * (up to 512 MB, or where twice as many can be seen as it has), or of those that sequences of max_kv positions can see through the
+ * (up to 512 MB, or where more than half as many can be seen), or of those that sequences of max_kv positions can see through the
  * window. Up to 4 GB; of a pool that would take more as bf16, up to 128 MB. Calls that see more take a way without copies, which for
  * prompts takes up to twice as long. */
 size_t sd2_attention_quantized_workspace_bytes(int32_t M, int32_t n_seq, int32_t H, int32_t Hkv, int32_t hd,
