@@ -490,7 +490,7 @@ sd2_status sd2_pages_append_quantized(const void* d_k, int64_t ldk, const void* 
  * if window is not 0. A NaN of the cache reaches the rows that see its position, no others. Of few rows, scores may lie
  * anywhere, also beyond fp32 (lse is infinite there); of prompts, q . k has to lie in fp32, with elements of q above 2^-110 (a row's
  * largest beyond it gives NaN). Which way a call takes goes by the query vectors (rows x heads per KV head) of its sequences, on average,
- * and by max_kv; probabilities are rounded to f16 in the ways of few vectors (by 2^-12), to bf16 in that of prompts (by 2^-9), so
+ * and by max_kv; probabilities are rounded to f16 in the ways of few vectors (by up to 2^-11), to bf16 in that of prompts (2^-8), so
  * that one sequence's last bits may change with the others of its batch. d_workspace:
  * sd2_attention_quantized_workspace_bytes(..) bytes, else as there; for prompts this includes a bf16 copy of pages: of the layer's
  * (up to 512 MB, or where more than half as many can be seen), or of those that sequences of max_kv positions can see through the
